@@ -315,6 +315,123 @@ int decoder_profile_read(pwd_decoder* dec, pwd_stage_times* out);
  * work of this handle is still running. */
 int decoder_destroy(pwd_decoder* dec);
 
+/* ---- Transformer operators ------------------------------------------------------------
+ * The products, the position rotation and the attention of a transformer layer over row-major
+ * tensors, for networks that the decoder's fused kernels do not hold. They have no handle: they
+ * run on the calling thread's current HIP device, whose memory every pointer must be, on
+ * hip_stream, and keep nothing from call to call. dtype is PWD_DTYPE_BF16 or PWD_DTYPE_F32; sums,
+ * softmax statistics and norms are fp32, results are rounded once. Strides and leading dimensions
+ * count elements, the last axis of every tensor is contiguous; rows may start at any element. A
+ * size of zero is a no-op. Outputs must not overlap inputs except where stated. Where a workspace
+ * size is given, it may be 0, and the caller allocates that many bytes of device memory (16-byte
+ * aligned, any contents) which calls that overlap must not share. PWD_EINVAL: a null pointer, a
+ * negative size, a stride smaller than the row it steps over, a workspace that is too small;
+ * PWD_EUNSUPPORTED: an unknown dtype or option, or a size outside the stated range. */
+
+/* Activations of pwd_linear: max(v, 0); v (1 + erf(v / sqrt 2)) / 2; v (1 + tanh(sqrt(2 / pi)
+ * (v + 0.044715 v^3))) / 2; v / (1 + exp(-v)). NaN stays NaN. */
+enum { PWD_ACT_NONE = 0, PWD_ACT_RELU = 1, PWD_ACT_GELU = 2, PWD_ACT_GELU_TANH = 3, PWD_ACT_SILU = 4 };
+
+/* y = act(x w^T + bias) + residual:
+ *   d_x [m][k] and d_w [n][k] (one row per output feature) of dtype; d_bias float [n] or NULL;
+ *   d_residual [m][n] or NULL and d_y [m][n] of out_dtype. m, n, k up to 2^31 - 512; k = 0 is an
+ * empty sum. d_y may be d_residual with the same leading dimension. A row's result depends on the
+ * other rows in its last bits at most: the order of the sum over k goes by m, n and k. */
+typedef struct {
+    int64_t m, n, k;
+    const void* d_x;
+    int64_t ld_x;
+    const void* d_w;
+    int64_t ld_w;
+    const float* d_bias;
+    const void* d_residual;
+    int64_t ld_residual;
+    void* d_y;
+    int64_t ld_y;
+    int32_t dtype, out_dtype, activation;
+    void* d_workspace;
+    size_t workspace_bytes;
+} pwd_linear_args;
+
+/* Workspace of a call with these sizes and dtype (the pointers are not looked at); 0 on bad arguments. */
+size_t pwd_linear_workspace(const pwd_linear_args* args);
+int pwd_linear(const pwd_linear_args* args, void* hip_stream);
+
+/* Rotation of query and key heads by position. A token has a position (int32, any sign) on each of
+ * `axes` axes (1..3; 0: none), d_positions [tokens][axes]. The first 2 P features of a head, P =
+ * pairs[0] + pairs[1] + pairs[2], are P pairs (u, v), dealt to the axes in turn; a pair becomes
+ * (u cos a - v sin a, u sin a + v cos a), a = position * frequency; the other features stay.
+ *   layout PWD_ROPE_HALF: pair j is features j and j + P; PWD_ROPE_ADJACENT: features 2 j and 2 j + 1.
+ *   frequencies PWD_ROPE_PER_AXIS: pair i of an axis with n pairs has theta^(-i / n);
+ *   PWD_ROPE_SHARED: pair j of all P has theta^(-j / P).
+ *   inverse: rotates by -a (the transpose, which undoes the rotation).
+ * d_q [tokens][q_heads][head_dim], d_k likewise with k_heads (0: no keys, the pointers are not looked
+ * at); the outputs have strides of their own and may be the inputs themselves with the same strides.
+ * head_dim even, 2..256; heads up to 65535. Angles are formed in double precision. */
+enum { PWD_ROPE_HALF = 0, PWD_ROPE_ADJACENT = 1 };
+enum { PWD_ROPE_PER_AXIS = 0, PWD_ROPE_SHARED = 1 };
+typedef struct {
+    int64_t tokens;
+    int32_t q_heads, k_heads, head_dim, dtype;
+    const void* d_q;
+    int64_t q_token_stride, q_head_stride;
+    const void* d_k;
+    int64_t k_token_stride, k_head_stride;
+    void* d_q_out;
+    int64_t q_out_token_stride, q_out_head_stride;
+    void* d_k_out;
+    int64_t k_out_token_stride, k_out_head_stride;
+    const int32_t* d_positions;
+    int32_t axes, pairs[3], layout, frequencies, inverse;
+    double theta;
+} pwd_rope_args;
+
+int pwd_rope(const pwd_rope_args* args, void* hip_stream);
+
+/* The same rotation after an RMS norm of every head over its features,
+ *   x <- gain * x / sqrt(mean(x^2) + eps),
+ * in one pass. d_gain_q, d_gain_k: float [head_dim], shared by the heads, or NULL (ones). eps >= 0.
+ * With axes = 0 the norm alone. */
+int pwd_qk_norm_rope(const pwd_rope_args* args, const float* d_gain_q, const float* d_gain_k, double eps,
+                     void* hip_stream);
+
+/* out = softmax(scale q k^T) v for every sequence of a batch and every query head; query head h reads
+ * key head h / (q_heads / k_heads). d_q, d_out [batch][q_len][q_heads][head_dim], d_k, d_v
+ * [batch][k_len][k_heads][head_dim], each with strides of batch, token and head.
+ *   d_q_lengths, d_k_lengths: int32 [batch] or NULL (q_len, k_len): how many queries and keys of each
+ *   sequence there are (values outside 0..q_len, 0..k_len count as the nearer end). What lies past them
+ *   is not used, whatever it holds, and output rows past them are left as they are.
+ *   Query i of a sequence stands at position k_length - q_length + i of its keys (the queries are the last
+ *   tokens) and sees the keys j of max(0, position - window_left) <= j <= position + window_right
+ *   (negative: no bound; window_right = 0 is causal) and the keys j < sinks up to position + window_right.
+ *   A query that sees no key gives zeros.
+ * head_dim up to 256, a multiple of 8 (bf16) or 4 (fp32); q_heads a multiple of k_heads; q_len, k_len up to
+ * 2^30; scale > 0. bf16: the weights are rounded to bf16 for their product with v. An infinite or NaN value
+ * in a row of v within the length may reach queries that do not see it. Results do not depend on the other sequences of the batch beyond their last bits: the keys are split
+ * over workgroups by the sizes of the call. */
+typedef struct {
+    int64_t batch, q_len, k_len;
+    int32_t q_heads, k_heads, head_dim, dtype;
+    const void* d_q;
+    int64_t q_stride[3];
+    const void* d_k;
+    int64_t k_stride[3];
+    const void* d_v;
+    int64_t v_stride[3];
+    void* d_out;
+    int64_t out_stride[3];
+    const int32_t* d_q_lengths;
+    const int32_t* d_k_lengths;
+    int64_t window_left, window_right, sinks;
+    double scale;
+    void* d_workspace;
+    size_t workspace_bytes;
+} pwd_attention_args;
+
+/* Workspace of a call with these sizes, dtype and window; 0 on bad arguments. */
+size_t pwd_attention_workspace(const pwd_attention_args* args);
+int pwd_attention(const pwd_attention_args* args, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,438 @@
+// y = act(x w^T + b) + r (pwd_linear): x [m][k], w [n][k], bf16 or fp32, sums in fp32.
+//
+// Both operands are contiguous along k, so both are read in 16-byte runs of k (a "chunk": 8 bf16
+// or 4 fp32 values) and the matrix core takes them as they lie: the product is computed as
+// y^T = w x^T with features along the rows of an MFMA tile and tokens along its columns, lane
+// (i = l % 16, g = l / 16) holding row or column i and chunk g of a k-step of four chunks. For bf16
+// that is one v_mfma_f32_16x16x32_bf16; for fp32 element e of the four chunks is the k-step of
+// v_mfma_f32_16x16x4_f32 number e (any order of k serves, as long as both operands share it).
+#include "common.h"
+#include "ops.h"
+#include "../../include/pwdec.h"
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes at any alignment of an element (the hardware splits a misaligned access)
+PWD_DEV u32x4 load16(const void* p) {
+    u32x4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+PWD_DEV void store16(void* p, u32x4 v) { __builtin_memcpy(p, &v, 16); }
+
+template <bool F32>
+PWD_DEV f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (F32) {
+        const f32x4 fa = __builtin_bit_cast(f32x4, a), fb = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[e], fb[e], c, 0, 0, 0);
+        return c;
+    } else {
+        return mfma16x16x32(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c);
+    }
+}
+
+// The chunk of `left` elements that remain at p (all of it, a part, or none): zeros past them.
+template <bool F32>
+PWD_DEV u32x4 load_chunk(const char* p, int left) {
+    constexpr int CH = F32 ? 4 : 8;
+    if (left >= CH) return load16(p);
+    u32x4 v = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < CH - 1; ++e)
+        if (e < left) {
+            if constexpr (F32) v[e] = reinterpret_cast<const uint32_t*>(p)[e];
+            else v[e >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[e] << (16 * (e & 1));
+        }
+    return v;
+}
+
+PWD_DEV float activate(float v, int act) {
+    switch (act) {
+        case PWD_ACT_RELU: return v < 0.f ? 0.f : v;
+        case PWD_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+        // 0.5 (1 + tanh u) = 1 / (1 + e^(-2u)); 2 sqrt(2 / pi) log2(e) = 2.3022082
+        case PWD_ACT_GELU_TANH:
+            return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.3022081981f * fmaf(0.044715f * v * v, v, v)));
+        case PWD_ACT_SILU: return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950409f * v));
+        default: return v;
+    }
+}
+
+// Adds the residual (if any) to NV consecutive outputs at (row, col) and stores them, rounded once
+// where the output is bf16. v holds act(sum + bias). Only columns < n exist.
+template <int NV>
+PWD_DEV void finish(const LinearParams& p, int64_t row, int col, const float* v) {
+    if (col >= p.n) return;
+    const bool whole = col + NV <= p.n;
+    const int64_t yo = row * p.ldy + col, ro = row * p.ldr + col;
+    float o[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) o[i] = v[i];
+    if (p.out_f32) {
+        float* y = static_cast<float*>(p.y) + yo;
+        const float* r = static_cast<const float*>(p.residual) + ro;
+        if (whole) {
+#pragma unroll
+            for (int j = 0; j < NV; j += 4) {
+                f32x4 u = {o[j], o[j + 1], o[j + 2], o[j + 3]};
+                if (p.residual) {
+                    const f32x4 q = __builtin_bit_cast(f32x4, load16(r + j));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) u[i] += q[i];
+                }
+                store16(y + j, __builtin_bit_cast(u32x4, u));
+            }
+        } else {
+            for (int i = 0; i < NV; ++i)
+                if (col + i < p.n) y[i] = o[i] + (p.residual ? r[i] : 0.f);
+        }
+    } else {
+        __bf16* y = static_cast<__bf16*>(p.y) + yo;
+        const __bf16* r = static_cast<const __bf16*>(p.residual) + ro;
+        if (whole) {
+            constexpr int B = NV >= 8 ? 8 : NV;
+            typedef __bf16 vec __attribute__((ext_vector_type(B)));
+#pragma unroll
+            for (int j = 0; j < NV; j += B) {
+                vec q, u;
+                if (p.residual) __builtin_memcpy(&q, r + j, sizeof q);
+#pragma unroll
+                for (int i = 0; i < B; ++i) u[i] = (__bf16)(p.residual ? o[j + i] + (float)q[i] : o[j + i]);
+                __builtin_memcpy(y + j, &u, sizeof u);
+            }
+        } else {
+            for (int i = 0; i < NV; ++i)
+                if (col + i < p.n) y[i] = (__bf16)(o[i] + (p.residual ? (float)r[i] : 0.f));
+        }
+    }
+}
+
+// bias of NV consecutive columns (0 past n or without a bias)
+template <int NV>
+PWD_DEV void load_bias(const LinearParams& p, int col, float* b) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) b[i] = p.bias && col + i < p.n ? p.bias[col + i] : 0.f;
+}
+
+// ---- tile kernel -------------------------------------------------------------------------
+//
+// A workgroup of WM x WN wavefronts owns BM tokens x BN features; a wavefront TT x FT MFMA tiles.
+// Stages of 128 bytes of k (64 bf16, 32 fp32) of the BM + BN rows are staged through two LDS
+// buffers: while stage s is multiplied, stage s + 1 arrives by direct loads (1 KB: 8 rows of 128
+// bytes, whole cache lines). Within a row the 16-byte chunk c sits at slot c ^ (row % 8), so that the
+// 16 rows of a fragment read spread over all banks. The features of a wavefront are dealt to its
+// FT tiles such that a lane's accumulators are 4 FT consecutive features: row r of tile f is feature
+// 4 FT (r / 4) + 4 f + r % 4, an order the loads apply when they fill the LDS rows.
+// DIRECT = false (rows that do not start on 16 bytes, or lie more than 4 GB apart within a tile) stages
+// through registers instead, as does the last stage where k ends inside it (zeros past the end).
+template <bool F32, int BM, int BN, int WM, int WN, bool DIRECT>
+__global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void linear_tile_kernel(LinearParams p, int tiles_m, int tiles_n) {
+    constexpr int NW = WM * WN, NT = NW * 64;
+    constexpr int TT = BM / WM / 16, FT = BN / WN / 16;
+    constexpr int ES = F32 ? 4 : 2, CH = 16 / ES, KSTAGE = 128 / ES;
+    constexpr int ROWS = BM + BN, UNITS = ROWS / 8, UPW = UNITS / NW;
+    constexpr int BUF = ROWS * 128;
+    constexpr int CPT = ROWS * 8 / NT;   // chunks of a stage per thread
+    static_assert(UNITS % NW == 0 && BM % 8 == 0, "whole units per wavefront");
+    extern __shared__ __align__(16) unsigned char lin_smem[];
+    unsigned char* smem = lin_smem;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = lane >> 4, col = lane & 15;
+    const int wm = wave % WM, wn = wave / WM;
+
+    // Workgroups go to the 8 XCDs in turn; each XCD takes a run of tiles, in columns of 8 token tiles,
+    // so that the tiles it works on at a time share rows in its L2.
+    const int nt = tiles_m * tiles_n, per = nt / 8, rest = nt % 8;
+    const int total = nt * p.splits;
+    int id = blockIdx.x % nt;
+    const int split = blockIdx.x / nt;
+    (void)total;
+    {
+        const int xcd = id % 8;
+        id = xcd * per + (xcd < rest ? xcd : rest) + id / 8;
+    }
+    constexpr int GM = 8;
+    const int group = id / (GM * tiles_n), first = group * GM;
+    const int gm = tiles_m - first < GM ? tiles_m - first : GM;
+    const int tm = first + (id - group * GM * tiles_n) % gm, tn = (id - group * GM * tiles_n) / gm;
+    const int64_t m0 = (int64_t)tm * BM;
+    const int n0 = tn * BN;
+
+    const char* xb = static_cast<const char*>(p.x) + m0 * p.ldx * ES;
+    const char* wb = static_cast<const char*>(p.w) + (int64_t)n0 * p.ldw * ES;
+    const int mleft = (int)(p.m - m0), nleft = p.n - n0;   // rows that exist from here on
+    auto feature = [&](int r) {   // feature (from n0) of LDS row r of the w tile
+        const int q = r % (16 * FT);
+        return r - q + (q % 16) / 4 * (4 * FT) + q / 16 * 4 + q % 4;
+    };
+    auto row_offset = [&](int r) -> int64_t {   // byte offset of LDS row r from xb or wb, within the tensor
+        if (r < BM) return (int64_t)(r < mleft ? r : mleft - 1) * p.ldx * ES;
+        const int f = feature(r - BM);
+        return (int64_t)(f < nleft ? f : nleft - 1) * p.ldw * ES;
+    };
+
+    const int stages_all = (p.k + KSTAGE - 1) / KSTAGE;
+    // stages of this split: runs of equal length, the first ones one longer
+    const int sq = stages_all / p.splits, sr = stages_all % p.splits;
+    const int s_begin = split * sq + (split < sr ? split : sr), s_end = s_begin + sq + (split < sr ? 1 : 0);
+
+    uint32_t voff[UPW];   // this lane's byte offset in each unit its wavefront loads
+    if constexpr (DIRECT) {
+#pragma unroll
+        for (int j = 0; j < UPW; ++j)
+            voff[j] = (uint32_t)row_offset((wave * UPW + j) * 8 + (lane >> 3)) + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
+    }
+    auto load_direct = [&](int s, int buf) {
+        const char* xs = xb + (int64_t)s * 128;
+        const char* ws = wb + (int64_t)s * 128;
+        const uint32_t dst = lds_addr(smem) + buf * BUF + wave * UPW * 1024;
+#pragma unroll
+        for (int j = 0; j < UPW; ++j) {
+            const char* src = (wave * UPW + j) * 8 < BM ? xs : ws;
+            asm volatile(LDS_DMA_GUARD "global_load_lds_dwordx4 %0, %1" :: "v"(voff[j]), "s"(src), "{m0}"(dst + j * 1024)
+                         : "memory");
+        }
+    };
+    u32x4 held[CPT];
+    auto load_held = [&](int s) {
+#pragma unroll
+        for (int j = 0; j < CPT; ++j) {
+            const int id2 = tid + j * NT, r = id2 >> 3, c = (id2 & 7) ^ (r & 7);
+            const int left = p.k - s * KSTAGE - c * CH;
+            const char* src = (r < BM ? xb : wb) + row_offset(r) + (int64_t)s * 128 + c * 16;
+            held[j] = load_chunk<F32>(src, left);
+        }
+    };
+    auto store_held = [&](int buf) {
+#pragma unroll
+        for (int j = 0; j < CPT; ++j) *reinterpret_cast<u32x4*>(smem + buf * BUF + (tid + j * NT) * 16) = held[j];
+    };
+    auto is_direct = [&](int s) { return DIRECT && (s + 1) * KSTAGE <= p.k; };
+
+    f32x4 acc[FT][TT];
+#pragma unroll
+    for (int f = 0; f < FT; ++f)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) acc[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    if (s_begin < s_end) {
+        if (is_direct(s_begin)) {
+            load_direct(s_begin, 0);
+        } else {
+            load_held(s_begin);
+            store_held(0);
+        }
+    }
+    for (int s = s_begin; s < s_end; ++s) {
+        const int buf = (s - s_begin) & 1;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();   // stage s is whole, and every wavefront is done with the other buffer
+        const bool more = s + 1 < s_end, direct = more && is_direct(s + 1);
+        if (direct) load_direct(s + 1, buf ^ 1);
+        else if (more) load_held(s + 1);
+        const unsigned char* xt = smem + buf * BUF + (wm * TT * 16 + col) * 128;
+        const unsigned char* wt = smem + buf * BUF + (BM + wn * FT * 16 + col) * 128;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            const int slot = ((ks * 4 + g) ^ (col & 7)) * 16;
+            u32x4 a[FT], b[TT];
+#pragma unroll
+            for (int f = 0; f < FT; ++f) a[f] = *reinterpret_cast<const u32x4*>(wt + f * 2048 + slot);
+#pragma unroll
+            for (int t = 0; t < TT; ++t) b[t] = *reinterpret_cast<const u32x4*>(xt + t * 2048 + slot);
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+#pragma unroll
+                for (int f = 0; f < FT; ++f) acc[f][t] = mma<F32>(a[f], b[t], acc[f][t]);
+        }
+        if (more && !direct) store_held(buf ^ 1);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // none is pending here; on every path, by its looks too
+
+    const int nc = n0 + wn * FT * 16 + g * 4 * FT;
+    if (p.partial) {   // sums of this split; linear_join_kernel adds them up and finishes
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            const int64_t row = m0 + wm * TT * 16 + t * 16 + col;
+            if (row >= p.m) continue;
+            float* o = p.partial + ((int64_t)split * p.m + row) * p.n + nc;
+#pragma unroll
+            for (int f = 0; f < FT; ++f) {
+                if (nc + 4 * f + 4 <= p.n) store16(o + 4 * f, __builtin_bit_cast(u32x4, acc[f][t]));
+                else
+                    for (int i = 0; i < 4; ++i)
+                        if (nc + 4 * f + i < p.n) o[4 * f + i] = acc[f][t][i];
+            }
+        }
+        return;
+    }
+    float bias[4 * FT];
+    load_bias<4 * FT>(p, nc, bias);
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        const int64_t row = m0 + wm * TT * 16 + t * 16 + col;
+        float v[4 * FT];
+#pragma unroll
+        for (int f = 0; f < FT; ++f)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[4 * f + i] = activate(acc[f][t][i] + bias[4 * f + i], p.act);
+        if (row < p.m) finish<4 * FT>(p, row, nc, v);
+    }
+}
+
+// Sum of the splits in their order, then bias, activation and residual: four outputs a thread.
+__global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
+    const int nq = (p.n + 3) / 4;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = id / nq;
+    if (row >= p.m) return;
+    const int c = (int)(id % nq) * 4;
+    float v[4] = {0.f, 0.f, 0.f, 0.f}, b[4];
+    load_bias<4>(p, c, b);
+    for (int s = 0; s < p.splits; ++s) {
+        const float* q = p.partial + ((int64_t)s * p.m + row) * p.n + c;
+        if (c + 4 <= p.n) {
+            const f32x4 u = __builtin_bit_cast(f32x4, load16(q));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += u[i];
+        } else {
+            for (int i = 0; i < 4; ++i)
+                if (c + i < p.n) v[i] += q[i];
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = activate(v[i] + b[i], p.act);
+    finish<4>(p, row, c, v);
+}
+
+// ---- few rows -----------------------------------------------------------------------------
+//
+// Up to 16 TB rows: the weights' bytes are what counts, each read once, so they go from memory
+// straight to the registers the matrix core reads, without LDS. A workgroup owns 16 features; its
+// NW wavefronts take runs of four k-steps (256 bytes of each of the 16 weight rows) in turn and add their
+// sums through LDS in the order of the wavefronts.
+template <bool F32, int TB, int NW>
+__global__ __launch_bounds__(NW * 64) void linear_rows_kernel(LinearParams p) {
+    constexpr int ES = F32 ? 4 : 2, CH = 16 / ES, KS = 4 * CH, RUN = 4 * KS;   // elements of a k-step, of a run
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
+    const int n0 = blockIdx.x * 16;
+    __shared__ __align__(16) float part[NW * TB * 256];
+    const int wr = n0 + col < p.n ? n0 + col : p.n - 1;
+    const char* wp = static_cast<const char*>(p.w) + (int64_t)wr * p.ldw * ES + g * 16;
+    const char* xp[TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) {
+        const int r = t * 16 + col;
+        xp[t] = static_cast<const char*>(p.x) + (int64_t)(r < p.m ? r : p.m - 1) * p.ldx * ES + g * 16;
+    }
+    f32x4 acc[TB];
+#pragma unroll
+    for (int t = 0; t < TB; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int runs = p.k / RUN;
+#pragma unroll 2
+    for (int r = wave; r < runs; r += NW) {
+        u32x4 a[4], b[TB][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) a[j] = load16(wp + (int64_t)r * (RUN * ES) + j * 64);
+#pragma unroll
+        for (int t = 0; t < TB; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[t][j] = load16(xp[t] + (int64_t)r * (RUN * ES) + j * 64);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int t = 0; t < TB; ++t) acc[t] = mma<F32>(a[j], b[t][j], acc[t]);
+    }
+    // what is left: fewer than four k-steps, the last of them possibly not whole
+    for (int j = wave; runs * RUN + j * KS < p.k; j += NW) {
+        const int k0 = runs * RUN + j * KS, left = p.k - k0 - g * CH;
+        const u32x4 a = load_chunk<F32>(wp + (int64_t)k0 * ES, left);
+#pragma unroll
+        for (int t = 0; t < TB; ++t) acc[t] = mma<F32>(a, load_chunk<F32>(xp[t] + (int64_t)k0 * ES, left), acc[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < TB; ++t) *reinterpret_cast<f32x4*>(part + ((wave * TB + t) * 64 + lane) * 4) = acc[t];
+    __syncthreads();
+    for (int i = tid; i < TB * 64; i += NW * 64) {
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const f32x4 q = *reinterpret_cast<const f32x4*>(part + (w * TB * 64 + i) * 4);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += q[e];
+        }
+        const int l = i & 63, row = (i >> 6) * 16 + (l & 15), c = n0 + 4 * (l >> 4);
+        if (row >= p.m || c >= p.n) continue;
+        float v[4], b[4];
+        load_bias<4>(p, c, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = activate(s[e] + b[e], p.act);
+        finish<4>(p, row, c, v);
+    }
+}
+
+template <bool F32, int TB, int NW>
+hipError_t rows(const LinearParams& p, hipStream_t s) {
+    linear_rows_kernel<F32, TB, NW><<<dim3((p.n + 15) / 16), dim3(NW * 64), 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <bool F32, int BM, int BN, int WM, int WN, bool DIRECT>
+hipError_t tile(const LinearParams& p, hipStream_t s) {
+    const int tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
+    const int smem = 2 * (BM + BN) * 128;
+    const void* fn = reinterpret_cast<const void*>(&linear_tile_kernel<F32, BM, BN, WM, WN, DIRECT>);
+    hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != hipSuccess) return e;
+    linear_tile_kernel<F32, BM, BN, WM, WN, DIRECT><<<dim3((uint32_t)tm * tn * p.splits), dim3(WM * WN * 64), smem, s>>>(p, tm, tn);
+    e = hipGetLastError();
+    if (e != hipSuccess || !p.partial) return e;
+    const int64_t threads = (int64_t)p.m * ((p.n + 3) / 4);
+    linear_join_kernel<<<dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <bool F32, bool DIRECT>
+hipError_t tiles(const LinearParams& p, int kernel, hipStream_t s) {
+    switch (kernel) {
+        case LIN_TILE256: return tile<F32, 256, 256, 2, 4, DIRECT>(p, s);
+        case LIN_TILE128: return tile<F32, 128, 128, 2, 2, DIRECT>(p, s);
+        default: return tile<F32, 64, 64, 2, 2, DIRECT>(p, s);
+    }
+}
+
+}  // namespace
+
+LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, bool f32, bool in_order) {
+    if (!in_order && m <= 64) return {m <= 16 ? LIN_ROWS16 : m <= 32 ? LIN_ROWS32 : LIN_ROWS64, 1};
+    auto tiles_of = [&](int64_t t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
+    if (tiles_of(256) >= 192) return {LIN_TILE256, 1};
+    if (tiles_of(128) >= 192) return {LIN_TILE128, 1};
+    return {LIN_TILE64, 1};
+}
+
+int64_t linear_threads(const LinearPlan& plan, int64_t m, int64_t n) {
+    const int64_t t = plan.kernel == LIN_TILE256 ? 256 : plan.kernel == LIN_TILE128 ? 128 : 64;
+    if (plan.kernel < LIN_TILE64) return (n + 15) / 16 * 512;
+    return (m + t - 1) / t * ((n + t - 1) / t) * plan.splits * (t == 256 ? 512 : 256);
+}
+
+hipError_t launch_linear(const LinearParams& p, const LinearPlan& plan, hipStream_t s) {
+    switch (plan.kernel) {
+        case LIN_ROWS16: return p.f32 ? rows<true, 1, 8>(p, s) : rows<false, 1, 8>(p, s);
+        case LIN_ROWS32: return p.f32 ? rows<true, 2, 8>(p, s) : rows<false, 2, 8>(p, s);
+        case LIN_ROWS64: return p.f32 ? rows<true, 4, 8>(p, s) : rows<false, 4, 8>(p, s);
+        default: break;
+    }
+    // direct loads copy 16-byte chunks from 32-bit offsets within a tile of up to 256 rows
+    const int es = p.f32 ? 4 : 2;
+    auto ok = [&](const void* q, int64_t ld) {
+        return reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld * es % 16 == 0 && ld * es <= (int64_t)15 << 20;
+    };
+    const bool direct = ok(p.x, p.ldx) && ok(p.w, p.ldw);
+    if (p.f32) return direct ? tiles<true, true>(p, plan.kernel, s) : tiles<true, false>(p, plan.kernel, s);
+    return direct ? tiles<false, true>(p, plan.kernel, s) : tiles<false, false>(p, plan.kernel, s);
+}

@@ -1,0 +1,444 @@
+// out = softmax(scale q k^T) v (pwd_attention): bf16 or fp32, key heads shared by groups of query heads,
+// sequences with their own lengths, a sliding window of keys and sinks.
+//
+// One pass over the keys with a running maximum and sum per query. The queries of a key head's group are
+// its rows: row r is token r / G, head r % G of the group (G query heads per key head), so that a tile
+// of keys and values is read once for the whole group, be it one new token or a prompt. Scores are
+// computed transposed, S^T = K Q^T: a row is a column of the MFMA tile (lane % 16), its keys lie along the
+// registers and the four lane groups, so a row's statistics cost one in-lane reduction and two lane
+// swaps, and the weights are the B operand of out^T = V^T P^T as they stand:
+//   bf16: two 16-key tiles make the 32-deep k-step with slots kslot(g, i) (common.h); V^T is staged in
+//         that key order. The weights are rounded to bf16 for that product (their sum is not).
+//   fp32: register e of a 16-key tile is the k-step of v_mfma_f32_16x16x4_f32 with keys 4 g + e, V as is.
+// Keys and values go global -> registers -> LDS, a tile ahead of the one that is multiplied, which lets
+// V be transposed on the way (four keys x 8 features a thread), rows start at any alignment and rows past
+// a sequence's keys be zeros whatever memory holds there. Only tiles that some row of the workgroup sees
+// are visited: the sinks' and the window's. Where rows are few, runs of those tiles go to different
+// workgroups (splits), whose sums mha_join_kernel joins in their order.
+#include "common.h"
+#include "ops.h"
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+PWD_DEV u32x4 load16(const void* p) {
+    u32x4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+
+template <bool F32, int DH, int NW, int QT>
+struct Shape {
+    static constexpr int ES = F32 ? 4 : 2, CH = 16 / ES;   // element bytes, elements of a 16-byte chunk
+    // keys of a tile: a single wavefront stages it all, which at 256 features fits its registers by half
+    static constexpr int KT = (F32 ? 32 : 64) / (NW == 1 && DH == 256 ? 2 : 1);
+    static constexpr int CK = DH / CH;                     // chunks of a row
+    static constexpr int KSQ = CK / 4;                     // k-steps of a score: four chunks
+    static constexpr int KB = KT * DH * ES, VB = KB;       // bytes of a tile of K, of V
+    static constexpr int BUFS = NW > 1 ? 2 : 1;            // several wavefronts: one barrier a tile
+    static constexpr int SMEM = BUFS * (KB + VB);
+    static constexpr int NT = NW * 64;
+    static constexpr int KL = KT * CK / NT;                // chunks of K a thread stages
+    static constexpr int VN = F32 ? KT * CK : KT / 4 * CK; // pieces of V: chunks, or blocks of 4 keys x 1 chunk
+    static constexpr int VL = (VN + NT - 1) / NT;          // of which a thread stages
+};
+
+// LDS slot (16 bytes) of chunk c of row r in a tile of rows of CK chunks
+template <int CK>
+PWD_DEV int slot_of(int r, int c) {
+    if constexpr (CK >= 8) return r * CK + (c ^ (r & 7));
+    else return r * CK + (c ^ ((r >> 1) & (CK - 1)));
+}
+// of V^T (bf16): row = feature, chunks of 8 keys; 8 features of one load differ in the low bits, the
+// loads' features in the next
+template <int KT>
+PWD_DEV int vt_slot(int f, int c) {
+    constexpr int N = KT / 8;
+    return f * N + (c ^ ((N == 8 ? f ^ (f >> 3) : (f >> 1) ^ (f >> 3)) & (N - 1)));
+}
+
+template <bool F32, int DH, int NW, int QT>
+__global__ __launch_bounds__(NW * 64) void mha_kernel(MhaParams p, int row_tiles) {
+    using S = Shape<F32, DH, NW, QT>;
+    constexpr int ES = S::ES, CH = S::CH, KT = S::KT, CK = S::CK, KSQ = S::KSQ, NT = S::NT;
+    constexpr int ST = KT / 16;          // 16-key tiles
+    constexpr int OT = DH / 16;          // feature tiles of the output
+    constexpr int ROWS = NW * QT * 16;
+    extern __shared__ __align__(16) unsigned char mha_smem[];
+    unsigned char* smem = mha_smem;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
+
+    // workgroup -> (sequence, key head, rows, split): the row tiles of one key head to one XCD (they read
+    // the same keys), the last rows first (under a causal mask they have the most to do)
+    const int total = gridDim.x, per = total / 8, rest = total % 8, xcd = blockIdx.x % 8;
+    int id = xcd * per + (xcd < rest ? xcd : rest) + blockIdx.x / 8;
+    const int split = id % p.splits;
+    id /= p.splits;
+    const int rt = row_tiles - 1 - id % row_tiles;
+    id /= row_tiles;
+    const int hk = id % p.k_heads, b = id / p.k_heads;
+    const int G = p.q_heads / p.k_heads;
+
+    int ql = p.q_lengths ? p.q_lengths[b] : p.q_len, kl = p.k_lengths ? p.k_lengths[b] : p.k_len;
+    ql = ql < 0 ? 0 : ql > p.q_len ? p.q_len : ql;
+    kl = kl < 0 ? 0 : kl > p.k_len ? p.k_len : kl;
+    const int64_t rows_all = (int64_t)ql * G, row0 = (int64_t)rt * ROWS;
+    if (row0 >= rows_all) return;
+    const int64_t row_end = row0 + ROWS < rows_all ? row0 + ROWS : rows_all;
+    // positions of the first and last token of the rows, and the keys that any of them sees
+    const int64_t p_lo = kl - ql + row0 / G, p_hi = kl - ql + (row_end - 1) / G;
+    auto clampk = [&](int64_t v) { return (int)(v < 0 ? 0 : v > kl ? kl : v); };
+    const int hi_any = p.right < 0 ? kl : clampk(p_hi + p.right + 1), hi_all = p.right < 0 ? kl : clampk(p_lo + p.right + 1);
+    const int lo_any = p.left < 0 ? 0 : clampk(p_lo - p.left), lo_all = p.left < 0 ? 0 : clampk(p_hi - p.left);
+    const int sink_end = p.sinks < lo_any ? (p.sinks < hi_any ? p.sinks : hi_any) : (lo_any < hi_any ? lo_any : hi_any);
+    const int sink_tiles = (sink_end + KT - 1) / KT;
+    const int first = lo_any / KT > sink_tiles ? lo_any / KT : sink_tiles, last = (hi_any + KT - 1) / KT;
+    const int ntiles = sink_tiles + (last > first ? last - first : 0);
+    const int tq = ntiles / p.splits, tr = ntiles % p.splits;
+    const int t_begin = split * tq + (split < tr ? split : tr), t_end = t_begin + tq + (split < tr ? 1 : 0);
+    auto key_of = [&](int t) { return (t < sink_tiles ? t : first + t - sink_tiles) * KT; };
+
+    // queries: B fragments, zeros past the head's features; the rows' windows
+    u32x4 qf[KSQ][QT];
+    int hi[QT], lo[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        const int64_t r = row0 + (wave * QT + t) * 16 + col;
+        const bool live = r < row_end;
+        const int64_t tok = (live ? r : row_end - 1) / G;
+        const int head = hk * G + (int)((live ? r : row_end - 1) % G);
+        const char* src = static_cast<const char*>(p.q) + (b * p.qs[0] + tok * p.qs[1] + head * p.qs[2]) * ES;
+#pragma unroll
+        for (int ks = 0; ks < KSQ; ++ks)
+            qf[ks][t] = (ks * 4 + g) * CH < p.dh ? load16(src + (ks * 4 + g) * 16) : u32x4{0, 0, 0, 0};
+        const int64_t pos = kl - ql + tok;
+        hi[t] = p.right < 0 ? kl : clampk(pos + p.right + 1);
+        lo[t] = p.left < 0 ? 0 : clampk(pos - p.left);
+    }
+
+    const char* kb = static_cast<const char*>(p.k) + (b * p.ks[0] + hk * p.ks[2]) * ES;
+    const char* vb = static_cast<const char*>(p.v) + (b * p.vs[0] + hk * p.vs[2]) * ES;
+    u32x4 kh[S::KL], vh[F32 ? S::VL : 4 * S::VL];
+    auto fetch = [&](int key0) {
+        auto chunk = [&](const char* base, int64_t stride, int key, int c) {
+            return key < kl && c * CH < p.dh ? load16(base + key * stride * ES + c * 16) : u32x4{0, 0, 0, 0};
+        };
+#pragma unroll
+        for (int j = 0; j < S::KL; ++j) {
+            const int i = tid + j * NT;
+            kh[j] = chunk(kb, p.ks[1], key0 + i / CK, i % CK);
+        }
+        if constexpr (F32) {
+#pragma unroll
+            for (int j = 0; j < S::VL; ++j) {
+                const int i = tid + j * NT;
+                vh[j] = chunk(vb, p.vs[1], key0 + i / CK, i % CK);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < S::VL; ++j) {
+                const int i = tid + j * NT;
+                if (S::VN % NT != 0 && i >= S::VN) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) vh[4 * j + e] = chunk(vb, p.vs[1], key0 + 4 * (i / CK) + e, i % CK);
+            }
+        }
+    };
+    auto stage = [&](unsigned char* at) {
+        unsigned char* vt = at + S::KB;
+#pragma unroll
+        for (int j = 0; j < S::KL; ++j) {
+            const int i = tid + j * NT;
+            *reinterpret_cast<u32x4*>(at + slot_of<CK>(i / CK, i % CK) * 16) = kh[j];
+        }
+        if constexpr (F32) {
+#pragma unroll
+            for (int j = 0; j < S::KL; ++j) {
+                const int i = tid + j * NT;
+                *reinterpret_cast<u32x4*>(vt + slot_of<CK>(i / CK, i % CK) * 16) = vh[j];
+            }
+        } else {
+            // block (4 keys, 8 features) -> per feature the 4 keys, at slots of key order
+#pragma unroll
+            for (int j = 0; j < S::VL; ++j) {
+                const int i = tid + j * NT;
+                if (S::VN % NT != 0 && i >= S::VN) break;
+                const int kblk = i / CK, f0 = (i % CK) * 8;
+                const int c = kblk / 8 * 4 + kblk % 4, half = kblk % 8 / 4;
+#pragma unroll
+                for (int f = 0; f < 8; ++f) {
+                    auto h = [&](int e) { return (vh[4 * j + e][f >> 1] >> (16 * (f & 1))) & 0xffffu; };
+                    const u32x2 w = {h(0) | h(1) << 16, h(2) | h(3) << 16};
+                    *reinterpret_cast<u32x2*>(vt + vt_slot<KT>(f0 + f, c) * 16 + half * 8) = w;
+                }
+            }
+        }
+    };
+
+    f32x4 acc[OT][QT];
+    float m[QT], l[QT];   // running maximum of the scaled scores (a lower bound within 2^8), this lane's part of the sum
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        m[t] = -__builtin_inff();
+        l[t] = 0.f;
+#pragma unroll
+        for (int o = 0; o < OT; ++o) acc[o][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    if (t_begin < t_end) fetch(key_of(t_begin));
+    for (int it = t_begin; it < t_end; ++it) {
+        unsigned char* at = smem + (S::BUFS > 1 ? ((it - t_begin) & 1) * (S::KB + S::VB) : 0);
+        if constexpr (S::BUFS == 1) __syncthreads();   // the previous tile has been read
+        stage(at);
+        __syncthreads();
+        const int key0 = key_of(it);
+        if (it + 1 < t_end) fetch(key_of(it + 1));
+        const unsigned char* vt = at + S::KB;
+
+        f32x4 s[ST][QT];
+#pragma unroll
+        for (int kt = 0; kt < ST; ++kt) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t) s[kt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int ks = 0; ks < KSQ; ++ks) {
+                const u32x4 a = *reinterpret_cast<const u32x4*>(at + slot_of<CK>(kt * 16 + col, ks * 4 + g) * 16);
+#pragma unroll
+                for (int t = 0; t < QT; ++t) {
+                    if constexpr (F32) {
+                        const f32x4 fa = __builtin_bit_cast(f32x4, a), fb = __builtin_bit_cast(f32x4, qf[ks][t]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[kt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[e], fb[e], s[kt][t], 0, 0, 0);
+                    } else {
+                        s[kt][t] = mfma16x16x32(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, qf[ks][t]), s[kt][t]);
+                    }
+                }
+            }
+        }
+        // scale; hide keys where the tile is not in sight of every row
+        const bool all = key0 + KT <= hi_all && (key0 >= lo_all || key0 + KT <= p.sinks);
+        float top[QT];
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            top[t] = -__builtin_inff();
+#pragma unroll
+            for (int kt = 0; kt < ST; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float v = s[kt][t][i] * p.scale2;
+                    if (!all) {
+                        const int key = key0 + kt * 16 + 4 * g + i;
+                        v = key < hi[t] && (key >= lo[t] || key < p.sinks) ? v : -__builtin_inff();
+                    }
+                    s[kt][t][i] = v;
+                    top[t] = fmaxf(top[t], v);
+                }
+        }
+        // the maximum moves only where some row's scores would exceed it by more than 2^8: the weights
+        // then stay below 2^8 and the sums far inside fp32, and most tiles leave the output as it is
+        bool grow = false;
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            top[t] = group_max(top[t]);
+            grow = grow || top[t] > m[t] + 8.f;
+        }
+        if (__builtin_amdgcn_ballot_w64(grow) != 0) {
+#pragma unroll
+            for (int t = 0; t < QT; ++t) {
+                const float mn = fmaxf(m[t], top[t]);
+                // a row that has seen no key yet (mn = -inf) keeps its zeros
+                const float c = mn > m[t] ? __builtin_amdgcn_exp2f(m[t] - mn) : 1.f;
+                m[t] = mn;
+                l[t] *= c;
+#pragma unroll
+                for (int o = 0; o < OT; ++o)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[o][t][i] *= c;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const float mt = m[t] == -__builtin_inff() ? 0.f : m[t];
+#pragma unroll
+            for (int kt = 0; kt < ST; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float w = __builtin_amdgcn_exp2f(s[kt][t][i] - mt);
+                    s[kt][t][i] = w;
+                    l[t] += w;
+                }
+        }
+        if constexpr (F32) {
+#pragma unroll
+            for (int kt = 0; kt < ST; ++kt)
+#pragma unroll
+                for (int o = 0; o < OT; ++o) {
+                    float a[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        a[e] = *reinterpret_cast<const float*>(vt + slot_of<CK>(kt * 16 + 4 * g + e, o * 4 + col / 4) * 16 + col % 4 * 4);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int t = 0; t < QT; ++t)
+                            acc[o][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], s[kt][t][e], acc[o][t], 0, 0, 0);
+                }
+        } else {
+#pragma unroll
+            for (int kp = 0; kp < ST / 2; ++kp) {
+                bf16x8 w[QT];
+#pragma unroll
+                for (int t = 0; t < QT; ++t) w[t] = pack_b(s[2 * kp][t], s[2 * kp + 1][t]);
+#pragma unroll
+                for (int o = 0; o < OT; ++o) {
+                    const u32x4 a = *reinterpret_cast<const u32x4*>(vt + vt_slot<KT>(o * 16 + col, kp * 4 + g) * 16);
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) acc[o][t] = mfma16x16x32(__builtin_bit_cast(bf16x8, a), w[t], acc[o][t]);
+                }
+            }
+        }
+    }
+
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+        const int64_t r = row0 + (wave * QT + t) * 16 + col;
+        const float sum = group_sum(l[t]);
+        if (r >= row_end) continue;
+        const int64_t tok = r / G;
+        const int head = hk * G + (int)(r % G);
+        if (p.splits > 1) {
+            const int64_t all_rows = (int64_t)p.batch * p.q_len * p.q_heads;
+            const int64_t row = (((int64_t)b * p.q_len + tok) * p.q_heads + head);
+            float* o = p.partial + ((int64_t)split * all_rows + row) * p.dh;
+#pragma unroll
+            for (int f = 0; f < OT; ++f)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (f * 16 + 4 * g + i < p.dh) o[f * 16 + 4 * g + i] = acc[f][t][i];
+            if (g == 0) {
+                float* ml = p.partial + (int64_t)p.splits * all_rows * p.dh + ((int64_t)split * all_rows + row) * 2;
+                ml[0] = m[t];
+                ml[1] = sum;
+            }
+        } else {
+            const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;   // a row that sees nothing: zeros
+            char* o = static_cast<char*>(p.out) + (b * p.os[0] + tok * p.os[1] + head * p.os[2]) * ES;
+#pragma unroll
+            for (int f = 0; f < OT; ++f) {
+                const int c = f * 16 + 4 * g;
+                if (c >= p.dh) continue;   // heads are whole multiples of 4 features
+                if constexpr (F32) {
+                    f32x4 v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = acc[f][t][i] * inv;
+                    __builtin_memcpy(o + c * 4, &v, 16);
+                } else {
+                    bf16x4 v;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = (__bf16)(acc[f][t][i] * inv);
+                    __builtin_memcpy(o + c * 2, &v, 8);
+                }
+            }
+        }
+    }
+}
+
+// Joins the splits of each row in their order: 64 lanes a row.
+template <bool F32>
+__global__ __launch_bounds__(256) void mha_join_kernel(MhaParams p) {
+    const int64_t all_rows = (int64_t)p.batch * p.q_len * p.q_heads;
+    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
+    if (row >= all_rows) return;
+    const int lane = threadIdx.x & 63;
+    const int head = (int)(row % p.q_heads);
+    const int64_t tok = row / p.q_heads % p.q_len;
+    const int b = (int)(row / p.q_heads / p.q_len);
+    if (p.q_lengths && tok >= p.q_lengths[b]) return;   // a row of padding stays as it is
+    const float* ml = p.partial + (int64_t)p.splits * all_rows * p.dh + row * 2;
+    float m = -__builtin_inff();
+    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, ml[s * all_rows * 2]);
+    const float mt = m == -__builtin_inff() ? 0.f : m;
+    float sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < p.splits; ++s) {
+        const float part = ml[s * all_rows * 2 + 1];
+        if (part == 0.f) continue;   // saw no key
+        const float w = __builtin_amdgcn_exp2f(ml[s * all_rows * 2] - mt);
+        sum = fmaf(part, w, sum);
+        const float* o = p.partial + (s * all_rows + row) * p.dh;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (lane + 64 * j < p.dh) v[j] = fmaf(o[lane + 64 * j], w, v[j]);
+    }
+    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+    const int64_t at = b * p.os[0] + tok * p.os[1] + head * p.os[2];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (lane + 64 * j < p.dh) {
+            if constexpr (F32) static_cast<float*>(p.out)[at + lane + 64 * j] = v[j] * inv;
+            else static_cast<__bf16*>(p.out)[at + lane + 64 * j] = (__bf16)(v[j] * inv);
+        }
+}
+
+template <bool F32, int DH, int NW, int QT>
+hipError_t go(const MhaParams& p, hipStream_t s) {
+    using S = Shape<F32, DH, NW, QT>;
+    const int64_t rows = (int64_t)p.q_len * (p.q_heads / p.k_heads);
+    const int row_tiles = (int)((rows + NW * QT * 16 - 1) / (NW * QT * 16));
+    const void* fn = reinterpret_cast<const void*>(&mha_kernel<F32, DH, NW, QT>);
+    hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    if (e != hipSuccess) return e;
+    mha_kernel<F32, DH, NW, QT><<<dim3((uint32_t)row_tiles * p.k_heads * p.batch * p.splits), dim3(NW * 64), S::SMEM, s>>>(p, row_tiles);
+    e = hipGetLastError();
+    if (e != hipSuccess || p.splits == 1) return e;
+    const int64_t all_rows = (int64_t)p.batch * p.q_len * p.q_heads;
+    mha_join_kernel<F32><<<dim3((uint32_t)((all_rows + 3) / 4)), dim3(256), 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <bool F32, int DH>
+hipError_t shapes(const MhaParams& p, const MhaPlan& plan, hipStream_t s) {
+    if (plan.waves == 1) return go<F32, DH, 1, 1>(p, s);
+    if constexpr (DH <= 128)
+        if (plan.tiles == 2) return go<F32, DH, 4, 2>(p, s);
+    return go<F32, DH, 4, 1>(p, s);
+}
+
+template <bool F32>
+hipError_t heads(const MhaParams& p, const MhaPlan& plan, hipStream_t s) {
+    if (p.dh <= 32) return shapes<F32, 32>(p, plan, s);
+    if (p.dh <= 64) return shapes<F32, 64>(p, plan, s);
+    if (p.dh <= 128) return shapes<F32, 128>(p, plan, s);
+    return shapes<F32, 256>(p, plan, s);
+}
+
+}  // namespace
+
+MhaPlan mha_plan(int64_t batch, int64_t q_len, int64_t k_len, int q_heads, int k_heads, int dh, int64_t left, int64_t right,
+                 int sinks, bool f32) {
+    MhaPlan pl;
+    const int64_t rows = q_len * (q_heads / k_heads);
+    pl.waves = rows <= 16 ? 1 : 4;
+    pl.tiles = rows <= 64 || dh > 128 ? 1 : 2;
+    const int64_t per = pl.waves * pl.tiles * 16, wgs = batch * k_heads * ((rows + per - 1) / per);
+    // keys that a workgroup visits, at most
+    const int KT = f32 ? 32 : 64;
+    int64_t keys = k_len;
+    if (left >= 0) {
+        const int64_t span = left + (right >= 0 ? right : k_len) + per + sinks + 2 * KT;
+        if (span < keys) keys = span;
+    }
+    const int64_t tiles = (keys + KT - 1) / KT;
+    int64_t splits = 1;
+    const int64_t want = pl.waves == 1 ? 1024 : 512;
+    if (wgs < want / 2) splits = want / (wgs > 0 ? wgs : 1);
+    if (splits > tiles / 4) splits = tiles / 4;
+    if (splits > 128) splits = 128;
+    pl.splits = splits < 1 ? 1 : (int)splits;
+    return pl;
+}
+
+hipError_t launch_mha(const MhaParams& p, const MhaPlan& plan, hipStream_t s) {
+    return p.f32 ? heads<true>(p, plan, s) : heads<false>(p, plan, s);
+}

@@ -14,11 +14,10 @@
 #include <vector>
 
 #include "../../include/pwdec.h"
+#include "host.h"
 #include "kernels.h"
 
-namespace {
-
-thread_local std::string g_last_error;
+static thread_local std::string g_last_error;
 
 int fail(int code, const char* fmt, ...) {
     char buf[512];
@@ -30,12 +29,7 @@ int fail(int code, const char* fmt, ...) {
     return code;
 }
 
-#define HIP_OK(call)                                                                     \
-    do {                                                                                 \
-        hipError_t e_ = (call);                                                          \
-        if (e_ != hipSuccess)                                                            \
-            return fail(PWD_EHIP, "%s failed: %s", #call, hipGetErrorString(e_));        \
-    } while (0)
+namespace {
 
 // Restores the caller's current device on scope exit.
 struct DeviceGuard {

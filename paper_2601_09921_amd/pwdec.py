@@ -50,6 +50,36 @@ class StageTimes(ctypes.Structure):
     _fields_ = [("ms", ctypes.c_double * NUM_STAGES), ("launches", ctypes.c_int64 * NUM_STAGES)]
 
 
+class LinearArgs(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64),
+                ("d_x", ctypes.c_void_p), ("ld_x", ctypes.c_int64), ("d_w", ctypes.c_void_p), ("ld_w", ctypes.c_int64),
+                ("d_bias", ctypes.c_void_p), ("d_residual", ctypes.c_void_p), ("ld_residual", ctypes.c_int64),
+                ("d_y", ctypes.c_void_p), ("ld_y", ctypes.c_int64),
+                ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32), ("activation", ctypes.c_int32),
+                ("d_workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class RopeArgs(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("q_heads", ctypes.c_int32), ("k_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32)] + \
+        [f for t in ("q", "k", "q_out", "k_out")
+         for f in ((f"d_{t}", ctypes.c_void_p), (f"{t}_token_stride", ctypes.c_int64), (f"{t}_head_stride", ctypes.c_int64))] + \
+        [("d_positions", ctypes.c_void_p), ("axes", ctypes.c_int32), ("pairs", ctypes.c_int32 * 3),
+         ("layout", ctypes.c_int32), ("frequencies", ctypes.c_int32), ("inverse", ctypes.c_int32),
+         ("theta", ctypes.c_double)]
+
+
+class AttentionArgs(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int64), ("q_len", ctypes.c_int64), ("k_len", ctypes.c_int64),
+                ("q_heads", ctypes.c_int32), ("k_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)] + \
+        [f for t, s in (("d_q", "q"), ("d_k", "k"), ("d_v", "v"), ("d_out", "out"))
+         for f in ((t, ctypes.c_void_p), (f"{s}_stride", ctypes.c_int64 * 3))] + \
+        [("d_q_lengths", ctypes.c_void_p), ("d_k_lengths", ctypes.c_void_p), ("window_left", ctypes.c_int64),
+         ("window_right", ctypes.c_int64), ("sinks", ctypes.c_int64), ("scale", ctypes.c_double),
+         ("d_workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
 _lib = None
 
 
@@ -82,6 +112,12 @@ def bind(lib: ctypes.CDLL) -> ctypes.CDLL:
         "decoder_profile": (ctypes.c_int, [VP, ctypes.c_int]),
         "decoder_schedule": (ctypes.c_int, [VP, ctypes.c_int]),
         "decoder_profile_read": (ctypes.c_int, [VP, P(StageTimes)]),
+        "pwd_linear_workspace": (ctypes.c_size_t, [P(LinearArgs)]),
+        "pwd_linear": (ctypes.c_int, [P(LinearArgs), VP]),
+        "pwd_rope": (ctypes.c_int, [P(RopeArgs), VP]),
+        "pwd_qk_norm_rope": (ctypes.c_int, [P(RopeArgs), VP, VP, ctypes.c_double, VP]),
+        "pwd_attention_workspace": (ctypes.c_size_t, [P(AttentionArgs)]),
+        "pwd_attention": (ctypes.c_int, [P(AttentionArgs), VP]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -309,3 +345,251 @@ class Decoder:
             self.close()
         except Exception:
             pass
+
+
+# ---- transformer operators (pwd_linear, pwd_rope, pwd_qk_norm_rope, pwd_attention)
+
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+ROPE_LAYOUTS = {"half": 0, "adjacent": 1}
+ROPE_FREQUENCIES = {"axis": 0, "shared": 1}
+_OP_DTYPES = {"float32": DTYPE_F32, "bfloat16": DTYPE_BF16}
+
+
+def _choice(value, table: dict, name: str) -> int:
+    if value not in table:
+        raise ValueError(f"{name}: {value!r}, need one of {', '.join(table)}")
+    return table[value]
+
+
+def _tensor(t, name: str, dims: int, like=None, dtypes: tuple = tuple(_OP_DTYPES), shape: tuple | None = None):
+    """Checks an operand of an operator: a CUDA tensor of `dims` axes whose last is contiguous, of one of
+    `dtypes`, of `shape` (None in it: any), on the device of `like`. Raises ValueError."""
+    if t is None or not getattr(t, "is_cuda", False):
+        raise ValueError(f"{name}: must be a CUDA tensor (got {getattr(t, 'device', t)})")
+    if like is not None and t.device.index != like.device.index:
+        raise ValueError(f"{name}: on cuda:{t.device.index}, need cuda:{like.device.index}")
+    if _dtype_names(t) not in dtypes:
+        raise ValueError(f"{name}: dtype {_dtype_names(t)}, need one of {', '.join(dtypes)}")
+    if t.dim() != dims or (shape is not None and any(s is not None and s != n for s, n in zip(shape, t.shape))):
+        need = tuple("any" if s is None else s for s in shape) if shape is not None else f"{dims} axes"
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, need {need}")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: its last axis must be contiguous (strides {tuple(t.stride())})")
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
+
+
+def _stride(t, axis: int, row: int) -> int:
+    """Stride of an axis, that of packed rows where it has one element (torch leaves it arbitrary)."""
+    return t.stride(axis) if t.shape[axis] != 1 else row
+
+
+def _span(t) -> tuple[int, int]:
+    """First and past-the-last address of a tensor's elements (none: an empty range)."""
+    if t.numel() == 0:
+        return 0, 0
+    last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
+    return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
+
+
+def _apart(out, name: str, *inputs):
+    """Refuses an output that lies over an input as a whole range of addresses (columns of one buffer
+    interleave and are the caller's to keep apart)."""
+    a, b = _span(out)
+    for t in inputs:
+        if t is None:
+            continue
+        c, d = _span(t)
+        dense = all(x.is_contiguous() for x in (out, t))
+        if a < d and c < b and (dense or a == c):
+            raise ValueError(f"{name}: overlaps an input")
+
+
+class _on:
+    """The operators' device and stream: the tensors' device made current, the given stream (which must
+    be of that device) or that device's current one."""
+
+    def __init__(self, t, stream):
+        import torch
+        self.guard = torch.cuda.device(t.device)
+        self.stream = torch.cuda.current_stream(t.device) if stream is None else stream
+        if stream is not None and stream.device.index != t.device.index:
+            raise ValueError(f"stream: of cuda:{stream.device.index}, the tensors are on cuda:{t.device.index}")
+
+    def __enter__(self):
+        self.guard.__enter__()
+        return ctypes.c_void_p(self.stream.cuda_stream)
+
+    def __exit__(self, *exc):
+        return self.guard.__exit__(*exc)
+
+
+def _workspace(need: int, given, like, stream):
+    """The caller's workspace (uint8, at least `need` bytes), or one from torch's allocator for the call's stream."""
+    if given is not None:
+        require(given, "workspace", ("uint8",), like.device.index, min_numel=need)
+        return given
+    if need == 0:
+        return None
+    import torch
+    if stream is None:
+        return torch.empty(need, dtype=torch.uint8, device=like.device)
+    with torch.cuda.stream(stream):   # the allocator reuses it in that stream's order
+        return torch.empty(need, dtype=torch.uint8, device=like.device)
+
+
+def linear(x, w, y, bias=None, activation: str = "none", residual=None, workspace=None, stream=None):
+    """y = activation(x w^T + bias) + residual. x: bfloat16 or float32 [m][k], w: the same type [n][k]
+    (one row per output feature); bias: float32 [n]; y: bfloat16 or float32 [m][n], residual of y's
+    type and shape (y itself allowed). Rows may be strided. activation: none, relu, gelu, gelu_tanh,
+    silu. workspace: uint8 cuda tensor of linear_workspace(...) bytes (None: taken from torch)."""
+    a = _linear_args(x, w, y, bias, activation, residual)
+    _apart(y, "y", x, w, bias, residual if residual is not None and residual.data_ptr() != y.data_ptr() else None)
+    lib = load_library()
+    with _on(x, stream) as s:
+        ws = _workspace(lib.pwd_linear_workspace(ctypes.byref(a)), workspace, x, stream)
+        if ws is not None:
+            a.d_workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+        _check(lib.pwd_linear(ctypes.byref(a), s))
+
+
+def _linear_args(x, w, y, bias, activation, residual) -> LinearArgs:
+    _tensor(x, "x", 2)
+    m, k = x.shape
+    _tensor(w, "w", 2, x, (_dtype_names(x),), (None, k))
+    n = w.shape[0]
+    _tensor(y, "y", 2, x, shape=(m, n))
+    if bias is not None:
+        _tensor(bias, "bias", 1, x, ("float32",), (n,))
+    if residual is not None:
+        _tensor(residual, "residual", 2, x, (_dtype_names(y),), (m, n))
+    return LinearArgs(m, n, k, _ptr(x), _stride(x, 0, k), _ptr(w), _stride(w, 0, k), _ptr(bias), _ptr(residual),
+                      _stride(residual, 0, n) if residual is not None else n, _ptr(y), _stride(y, 0, n),
+                      _OP_DTYPES[_dtype_names(x)], _OP_DTYPES[_dtype_names(y)],
+                      _choice(activation, ACTIVATIONS, "activation"))
+
+
+def linear_workspace(x, w, y) -> int:
+    """Bytes of workspace that linear takes for these operands."""
+    return load_library().pwd_linear_workspace(ctypes.byref(_linear_args(x, w, y, None, "none", None)))
+
+
+def _rope_args(q, k, positions, pairs, theta, layout, frequencies, inverse, q_out, k_out):
+    ref = q if q is not None else k
+    if ref is None:
+        raise ValueError("rope: q or k is required")
+    _tensor(ref, "q" if q is not None else "k", 3)
+    tokens, _, dh = ref.shape
+    dt = (_dtype_names(ref),)
+    if k is not None:
+        _tensor(k, "k", 3, ref, dt, (tokens, None, dh))
+    if (q_out is not None and q is None) or (k_out is not None and k is None):
+        raise ValueError("rope: an output without its input")
+    outs = []
+    for t, o, name in ((q, q_out, "q_out"), (k, k_out, "k_out")):
+        o = t if o is None else o
+        if t is not None:
+            _tensor(o, name, 3, ref, dt, tuple(t.shape))
+            if o.data_ptr() == t.data_ptr() and o.stride() != t.stride() and t.numel():
+                raise ValueError(f"{name}: in place needs the same strides")
+            if o.data_ptr() != t.data_ptr():
+                _apart(o, name, q, k)
+        outs.append(o)
+    pairs = tuple(int(p) for p in pairs)
+    if len(pairs) > 3:
+        raise ValueError(f"pairs: {len(pairs)} axes, need at most 3")
+    if positions is not None and positions.dim() == 1:
+        positions = positions[:, None]
+    if pairs:
+        _tensor(positions, "positions", 2, ref, ("int32",), (tokens, len(pairs)))
+        if not positions.is_contiguous():
+            raise ValueError("positions: must be contiguous")
+    elif positions is not None:
+        raise ValueError("positions: given without pairs")
+    a = RopeArgs(tokens, q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0, dh, _OP_DTYPES[dt[0]])
+    for name, t in (("q", q), ("k", k), ("q_out", outs[0]), ("k_out", outs[1])):
+        if t is not None:
+            setattr(a, f"d_{name}", t.data_ptr())
+            setattr(a, f"{name}_head_stride", _stride(t, 1, dh))
+            setattr(a, f"{name}_token_stride", _stride(t, 0, dh * t.shape[1]))
+    a.d_positions, a.axes = _ptr(positions), len(pairs)
+    a.pairs = (ctypes.c_int32 * 3)(*pairs)
+    a.layout = _choice(layout, ROPE_LAYOUTS, "layout")
+    a.frequencies = _choice(frequencies, ROPE_FREQUENCIES, "frequencies")
+    a.inverse, a.theta = int(bool(inverse)), float(theta)
+    return a, ref
+
+
+def rope(q, k, positions, pairs, theta: float = 10000.0, layout: str = "half", frequencies: str = "axis",
+         inverse: bool = False, q_out=None, k_out=None, stream=None):
+    """Rotates the heads of q [tokens][q_heads][dh] and k [tokens][k_heads][dh] (either may be None;
+    bfloat16 or float32) by their tokens' positions, int32 [tokens][axes] (or [tokens]), in place or into
+    q_out / k_out. pairs: feature pairs of each axis. layout: half (pair j is features j and j + P) or
+    adjacent (2 j and 2 j + 1); frequencies: axis (theta^(-i / pairs of the axis)) or shared
+    (theta^(-j / P)); inverse: undo the rotation."""
+    a, ref = _rope_args(q, k, positions, pairs, theta, layout, frequencies, inverse, q_out, k_out)
+    with _on(ref, stream) as s:
+        _check(load_library().pwd_rope(ctypes.byref(a), s))
+
+
+def qk_norm_rope(q, k, gain_q, gain_k, positions, pairs, theta: float = 10000.0, layout: str = "half",
+                 frequencies: str = "axis", eps: float = 1e-6, q_out=None, k_out=None, stream=None):
+    """RMS norm of every head of q and k (gains float32 [dh], or None), then the rotation of rope, in
+    one pass. pairs = () and positions = None: the norm alone."""
+    a, ref = _rope_args(q, k, positions, pairs, theta, layout, frequencies, False, q_out, k_out)
+    for gain, name in ((gain_q, "gain_q"), (gain_k, "gain_k")):
+        if gain is not None:
+            _tensor(gain, name, 1, ref, ("float32",), (ref.shape[2],))
+    with _on(ref, stream) as s:
+        _check(load_library().pwd_qk_norm_rope(ctypes.byref(a), ctypes.c_void_p(_ptr(gain_q)),
+                                               ctypes.c_void_p(_ptr(gain_k)), float(eps), s))
+
+
+def _attention_args(q, k, v, out, window, sinks, scale, q_lengths, k_lengths) -> AttentionArgs:
+    _tensor(q, "q", 4)
+    b, sq, hq, dh = q.shape
+    dt = (_dtype_names(q),)
+    _tensor(k, "k", 4, q, dt, (b, None, None, dh))
+    _tensor(v, "v", 4, q, dt, tuple(k.shape))
+    _tensor(out, "out", 4, q, dt, tuple(q.shape))
+    for t, name in ((q_lengths, "q_lengths"), (k_lengths, "k_lengths")):
+        if t is not None:
+            _tensor(t, name, 1, q, ("int32",), (b,))
+    a = AttentionArgs(b, sq, k.shape[1], hq, k.shape[2], dh, _OP_DTYPES[dt[0]])
+    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
+        setattr(a, f"d_{name}", _ptr(t))
+        head = _stride(t, 2, dh)
+        token = _stride(t, 1, dh * t.shape[2])
+        setattr(a, f"{name}_stride", (ctypes.c_int64 * 3)(_stride(t, 0, dh * t.shape[2] * t.shape[1]), token, head))
+    a.d_q_lengths, a.d_k_lengths = _ptr(q_lengths), _ptr(k_lengths)
+    a.window_left, a.window_right = (int(n) for n in window)
+    a.sinks = int(sinks)
+    a.scale = float(scale) if scale is not None else dh ** -0.5
+    return a
+
+
+def attention(q, k, v, out, window=(-1, -1), sinks: int = 0, scale: float | None = None, q_lengths=None,
+              k_lengths=None, workspace=None, stream=None):
+    """out = softmax(scale q k^T) v. q, out: bfloat16 or float32 [batch][q_len][q_heads][dh]; k, v:
+    [batch][k_len][k_heads][dh], q_heads a multiple of k_heads; rows may be strided. window = (left,
+    right): keys before and after a query's own position that it sees (-1: all; right = 0: causal), besides
+    the first `sinks` keys. q_lengths / k_lengths: int32 [batch], the queries and keys of each sequence; the
+    queries are its last tokens, and output rows past them are left as they are. A query that sees no
+    key gives zeros. scale: dh^-0.5 by default. workspace: uint8 cuda tensor of
+    attention_workspace(...) bytes (None: taken from torch)."""
+    a = _attention_args(q, k, v, out, window, sinks, scale, q_lengths, k_lengths)
+    _apart(out, "out", q, k, v)
+    lib = load_library()
+    with _on(q, stream) as s:
+        ws = _workspace(lib.pwd_attention_workspace(ctypes.byref(a)), workspace, q, stream)
+        if ws is not None:
+            a.d_workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
+        _check(lib.pwd_attention(ctypes.byref(a), s))
+
+
+def attention_workspace(q, k, v, out, window=(-1, -1), sinks: int = 0) -> int:
+    """Bytes of workspace that attention takes for these operands."""
+    return load_library().pwd_attention_workspace(
+        ctypes.byref(_attention_args(q, k, v, out, window, sinks, None, None, None)))
