@@ -315,6 +315,38 @@ int decoder_profile_read(pwd_decoder* dec, pwd_stage_times* out);
  * work of this handle is still running. */
 int decoder_destroy(pwd_decoder* dec);
 
+/* ---- Rotary networks ----
+ * The decoder's network with another attention, on the operators below instead of the fused kernels, and
+ * so for more widths: the position scheme is a rotation of queries and keys by the token's row and
+ * column on the (d+1)x(d+1) lattice (pwd_rope's half layout, per-axis frequencies) in place of the
+ * sinusoidal encoding of the embedding, each head of Q and K may take an RMS norm first, and a token may
+ * see a window of the tokens around it in row-major order and the first `sinks` tokens only.
+ *   pairs: feature pairs of each head turned by the row and by the column; both 0: no rotation, and the
+ *   sinusoidal encoding stays. theta: base of the frequencies. qk_norm: 0 or 1, with norm_eps.
+ *   window: tokens before and after that a token sees, -1: all (sinks is then not looked at).
+ * Supported: geometry as for decoder_validate_config without its on-chip limits, max_windows *
+ * max(n_tokens, distance^2) * max(d_model, 64) below 2^32; PWD_DTYPE_BF16 or PWD_DTYPE_F32; d_model a multiple of 16 in 16..1024 and a head size
+ * that is a multiple of 8 (bf16) or 4 (fp32) up to 256 (d_model 192 with 8 heads of 24, the
+ * hyperparameter table's, among them); mlp_ratio, n_layers, token_set, embedder as there; no dilated
+ * convolutions. The entry points of the handle are the same; it has the one schedule
+ * PWD_SCHEDULE_LAYERS, and the stages of decoder_profile are: EMBED_QKV the embedding and fold, POST_QKV
+ * the Q/K/V projection with norm and rotation, ATTENTION, OUT_PROJ, POST the feed-forward, READOUT.
+ * Blob: header word 14 = qk_norm | pairs[0] << 8 | pairs[1] << 16, word 15 = theta (float32 bits);
+ * with qk_norm the tensors gq[head size] gk[head size] of every layer follow all others. */
+typedef struct {
+    int32_t pairs[2];
+    float theta;
+    int32_t qk_norm;
+    float norm_eps;
+    int32_t window;
+    int32_t sinks;
+} pwd_rotary_dims;
+
+size_t decoder_rotary_blob_floats(const pwd_geometry* geom, const pwd_model_dims* dims, const pwd_rotary_dims* rotary);
+int decoder_validate_rotary(const pwd_geometry* geom, const pwd_model_dims* dims, const pwd_rotary_dims* rotary);
+int decoder_create_rotary(const pwd_geometry* geom, const pwd_model_dims* dims, const pwd_rotary_dims* rotary,
+                          const void* weight_blob, size_t blob_bytes, pwd_decoder** out);
+
 /* ---- Transformer operators ------------------------------------------------------------
  * The products, the position rotation and the attention of a transformer layer over row-major
  * tensors, for networks that the decoder's fused kernels do not hold. They have no handle: they

@@ -171,3 +171,54 @@ struct StreamCombineParams {
 };
 hipError_t launch_stream_split(const StreamSplitParams& p, hipStream_t s);
 hipError_t launch_stream_combine(const StreamCombineParams& p, hipStream_t s);
+
+// ---- rotary networks: the decoder's row-major stages around the operators (rotary.hip)
+
+// X = kappa (S_t + X) over [nwin * ntok][D] (X = kappa S_0 at t = 0), with a bf16 copy if Xb.
+struct FoldParams {
+    SyndromeIn in;
+    int ntok, t, D;
+    const int* tok_stab;    // stabilizer of each token or -1; null: token s = stabilizer s
+    const float* S0;        // [ntok][D]: b_e (+ PE)
+    const float* we;        // [D]
+    const int* emb_nb;      // embedder's residual block (TokParams), or null
+    const float* emb_tab;
+    float kappa;
+    float* X;
+    uint16_t* Xb;
+};
+hipError_t launch_fold(const FoldParams& p, hipStream_t s);
+
+// LayerNorm of the rows of X in place, with a bf16 copy if Xb.
+struct NormParams {
+    float* X;
+    uint16_t* Xb;
+    const float *gamma, *beta;
+    int64_t rows;
+    int D;
+    float eps;
+};
+hipError_t launch_row_norm(const NormParams& p, hipStream_t s);
+
+// The 2x2 neighbourhoods of the readout: G [nwin * d * d][4][D] (zeros at cells without a token), fp32 or bf16.
+struct GatherParams {
+    const float* X;
+    void* G;
+    const int* cell_token;
+    int nwin, d, ntok, D;
+    bool f32;
+};
+hipError_t launch_gather(const GatherParams& p, hipStream_t s);
+
+// logit = <w_o, mean over columns of Y> + b_o + beta[type] with Y [nwin][d][d][D] (after the ReLU).
+struct PoolParams {
+    const float* Y;
+    const float* wo;        // [d][D]
+    const uint8_t* types;
+    float bo, beta[3];
+    float* logits;
+    uint8_t* bits;
+    int* err;
+    int nwin, d, D, stride;
+};
+hipError_t launch_pool(const PoolParams& p, hipStream_t s);

@@ -16,6 +16,7 @@
 #include "../../include/pwdec.h"
 #include "host.h"
 #include "kernels.h"
+#include "ops.h"
 
 static thread_local std::string g_last_error;
 
@@ -293,6 +294,11 @@ size_t conv_floats(const pwd_model_dims* m) {
     return has_conv(m) ? (size_t)m->n_layers * (27 * D * D + 3 * D) : 0;
 }
 
+// blob floats of a rotary network's norm gains (the last tensors)
+size_t rotary_floats(const pwd_model_dims* m, const pwd_rotary_dims* r) {
+    return r->qk_norm ? (size_t)m->n_layers * 2 * (m->d_model / m->n_heads) : 0;
+}
+
 // The embedder's residual block (model table: 2 x Conv1d(D, D) after Linear(1 -> D); the
 // syndrome-convolution section puts it on the flattened (d+1)^2 array ahead of PE) as a
 // lookup. Its input at cell q is E(q) = e_q w_e + b_e, one event bit lifted to D features,
@@ -427,11 +433,50 @@ struct pwd_decoder {
     const uint16_t* res_stream = nullptr;
     const float* res_vecs = nullptr;
     float bo_out = 0.f, beta[3] = {0.f, 0.f, 0.f};
+    // rotary networks (decoder_create_rotary): row-major weights [out][in] and activations
+    bool rotary = false;
+    pwd_rotary_dims rot{};
+    struct RotaryLayer {
+        const void *wqkv, *wo, *w1, *w2;
+        const float *bqkv, *bo, *g1, *be1, *b1, *b2, *g2, *be2, *gq, *gk;
+    };
+    std::vector<RotaryLayer> rlayers;
+    const void* rot_wc = nullptr;          // readout convolution [D][4 D]
+    const int32_t* rot_pos = nullptr;      // (row, column) of every token of max_windows windows
+    void* rot_act = nullptr;               // activations of max_windows windows
     // per-stage timing (decoder_profile)
     bool profiling = false;
     struct Mark { hipEvent_t begin, end; int stage; };
     std::vector<Mark> marks;       // recorded, not yet read
     std::vector<hipEvent_t> spare; // released events for reuse
+};
+
+// A rotary network's activations of n windows, cut out of one allocation at `base`.
+struct RotaryBuffers {
+    float* X;        // [rows][D] residual stream and recurrent state
+    uint16_t* Xb;    // its bf16 copy (fp32 networks: none)
+    void* QKV;       // [rows][3 D]; the readout's convolution output [n d d][D] fp32
+    void* A;         // [rows][D] attention output
+    void* H;         // [rows][F] hidden units; the readout's neighbourhoods [n d d][4 D]
+    size_t bytes;
+    RotaryBuffers(const pwd_decoder* dec, int64_t n, void* base) {
+        const bool f32 = dec->dtype == PWD_DTYPE_F32;
+        const size_t es = f32 ? 4 : 2, rows = (size_t)n * dec->ntok, D = dec->D, cells = (size_t)n * dec->d * dec->d;
+        unsigned char* b = static_cast<unsigned char*>(base);
+        size_t at = 0;
+        auto take = [&](size_t want) {
+            void* p = b ? b + at : nullptr;
+            at += (want + 255) & ~(size_t)255;
+            return p;
+        };
+        X = static_cast<float*>(take(rows * D * 4));
+        Xb = static_cast<uint16_t*>(take(f32 ? 0 : rows * D * 2));
+        if (f32) Xb = nullptr;
+        QKV = take(std::max(rows * 3 * D * es, cells * D * 4));
+        A = take(rows * D * es);
+        H = take(std::max(rows * dec->F, cells * 4 * D) * es);
+        bytes = at;
+    }
 };
 
 namespace {
@@ -474,7 +519,8 @@ size_t decoder_blob_floats(const pwd_geometry* geom, const pwd_model_dims* dims)
            (size_t)d * D + 1 + 3 + res_floats(dims) + conv_floats(dims);
 }
 
-int decoder_validate_config(const pwd_geometry* g, const pwd_model_dims* m) {
+// Checks of the geometry and of the options that every kind of network shares.
+static int validate_common(const pwd_geometry* g, const pwd_model_dims* m) {
     if (!g || !m) return fail(PWD_EINVAL, "null geometry or dimensions");
     const int d = g->distance;
     // any odd distance whose attention tile (bf16) or window (fp32) fits on chip, checked below
@@ -488,7 +534,6 @@ int decoder_validate_config(const pwd_geometry* g, const pwd_model_dims* m) {
     if (m->n_layers < 1 || m->n_layers > 8) return fail(PWD_EUNSUPPORTED, "n_layers %d: need 1..8", m->n_layers);
     if (m->n_heads < 1 || m->d_model % m->n_heads != 0)
         return fail(PWD_EUNSUPPORTED, "d_model %d not divisible by n_heads %d", m->d_model, m->n_heads);
-    const int dh = m->d_model / m->n_heads;
     if (m->token_set != PWD_TOKENS_STABILIZERS && m->token_set != PWD_TOKENS_GRID)
         return fail(PWD_EUNSUPPORTED, "token_set %d: need 0 (stabilizers) or 1 (grid)", m->token_set);
     if (m->embedder != PWD_EMBED_LINEAR && m->embedder != PWD_EMBED_RESNET)
@@ -503,6 +548,13 @@ int decoder_validate_config(const pwd_geometry* g, const pwd_model_dims* m) {
         if (m->dtype == PWD_DTYPE_MXFP8)
             return fail(PWD_EUNSUPPORTED, "MXFP8 networks without the dilated convolutions only");
     }
+    return PWD_OK;
+}
+
+int decoder_validate_config(const pwd_geometry* g, const pwd_model_dims* m) {
+    const int rc = validate_common(g, m);
+    if (rc != PWD_OK) return rc;
+    const int d = g->distance, dh = m->d_model / m->n_heads;
     const int N = m->token_set == PWD_TOKENS_GRID ? (d + 1) * (d + 1) : d * d - 1;   // tokens
     if (m->dtype == PWD_DTYPE_BF16 || m->dtype == PWD_DTYPE_MXFP8) {
         if (m->d_model != 128 && m->d_model != 256)
@@ -525,12 +577,64 @@ int decoder_validate_config(const pwd_geometry* g, const pwd_model_dims* m) {
     return PWD_OK;
 }
 
+static int create_decoder(const pwd_geometry* geom, const pwd_model_dims* dims, const pwd_rotary_dims* rot, const void* blob,
+                          size_t blob_bytes, pwd_decoder** out);
+
 int decoder_create(const pwd_geometry* geom, const pwd_model_dims* dims, const void* blob,
                    size_t blob_bytes, pwd_decoder** out) {
     if (!out || !blob) return fail(PWD_EINVAL, "null blob or output handle");
-    int rc = decoder_validate_config(geom, dims);
+    const int rc = decoder_validate_config(geom, dims);
+    return rc != PWD_OK ? rc : create_decoder(geom, dims, nullptr, blob, blob_bytes, out);
+}
+
+size_t decoder_rotary_blob_floats(const pwd_geometry* geom, const pwd_model_dims* dims, const pwd_rotary_dims* rotary) {
+    if (!geom || !dims || !rotary || dims->n_heads < 1) return 0;
+    return decoder_blob_floats(geom, dims) + rotary_floats(dims, rotary);
+}
+
+int decoder_validate_rotary(const pwd_geometry* g, const pwd_model_dims* m, const pwd_rotary_dims* r) {
+    if (!r) return fail(PWD_EINVAL, "null rotary options");
+    const int rc = validate_common(g, m);
     if (rc != PWD_OK) return rc;
-    const size_t nf = decoder_blob_floats(geom, dims);
+    if (m->dtype != PWD_DTYPE_F32 && m->dtype != PWD_DTYPE_BF16)
+        return fail(PWD_EUNSUPPORTED, "rotary network of dtype %d: need 0 (fp32) or 1 (bf16)", m->dtype);
+    if (has_conv(m)) return fail(PWD_EUNSUPPORTED, "rotary networks without the dilated convolutions only");
+    if (m->d_model < 16 || m->d_model > 1024 || m->d_model % 16 != 0)
+        return fail(PWD_EUNSUPPORTED, "rotary d_model %d: need a multiple of 16 in 16..1024", m->d_model);
+    const int dh = m->d_model / m->n_heads, unit = m->dtype == PWD_DTYPE_F32 ? 4 : 8;
+    if (dh % unit != 0 || dh > 256)
+        return fail(PWD_EUNSUPPORTED, "rotary head size %d: need a multiple of %d up to 256", dh, unit);
+    const int64_t ntok = m->token_set == PWD_TOKENS_GRID ? (g->distance + 1) * (g->distance + 1) : g->distance * g->distance - 1;
+    // one launch's threads: a row takes up to d_model of them, and 64 at least
+    const int64_t rows = std::max(ntok, (int64_t)g->distance * g->distance) * g->max_windows;
+    if (rows * std::max(m->d_model, 64) >= (int64_t)1 << 32)
+        return fail(PWD_EUNSUPPORTED, "%d windows of %lld tokens x %d: need fewer than 2^32 features in all", g->max_windows,
+                    (long long)ntok, m->d_model);
+    for (int i = 0; i < 2; ++i)
+        if (r->pairs[i] < 0 || r->pairs[i] > dh / 2)
+            return fail(PWD_EINVAL, "rotary pairs[%d] = %d in heads of %d", i, r->pairs[i], dh);
+    if (r->pairs[0] + r->pairs[1] > dh / 2)
+        return fail(PWD_EINVAL, "rotary pairs %d + %d in heads of %d", r->pairs[0], r->pairs[1], dh);
+    if (!(r->theta > 0.f) || !std::isfinite(r->theta)) return fail(PWD_EINVAL, "rotary theta %g: need a positive number", r->theta);
+    if (r->qk_norm != 0 && r->qk_norm != 1) return fail(PWD_EUNSUPPORTED, "qk_norm %d: need 0 or 1", r->qk_norm);
+    if (!(r->norm_eps >= 0.f) || !std::isfinite(r->norm_eps)) return fail(PWD_EINVAL, "norm_eps %g: need at least 0", r->norm_eps);
+    if (r->window < -1 || (r->window >= 0 && r->sinks < 0))
+        return fail(PWD_EINVAL, "window %d, sinks %d: need at least -1, 0", r->window, r->sinks);
+    return PWD_OK;
+}
+
+int decoder_create_rotary(const pwd_geometry* geom, const pwd_model_dims* dims, const pwd_rotary_dims* rotary,
+                          const void* blob, size_t blob_bytes, pwd_decoder** out) {
+    if (!out || !blob) return fail(PWD_EINVAL, "null blob or output handle");
+    const int rc = decoder_validate_rotary(geom, dims, rotary);
+    return rc != PWD_OK ? rc : create_decoder(geom, dims, rotary, blob, blob_bytes, out);
+}
+
+// The handle of a network whose configuration has been checked (rot: null, or a rotary network's options).
+static int create_decoder(const pwd_geometry* geom, const pwd_model_dims* dims, const pwd_rotary_dims* rot, const void* blob,
+                          size_t blob_bytes, pwd_decoder** out) {
+    int rc = PWD_OK;
+    const size_t nf = decoder_blob_floats(geom, dims) + (rot ? rotary_floats(dims, rot) : 0);
     if (blob_bytes != PWD_BLOB_HEADER_WORDS * 4 + nf * 4)
         return fail(PWD_EBLOB, "blob has %zu bytes, expected %zu", blob_bytes, PWD_BLOB_HEADER_WORDS * 4 + nf * 4);
     uint32_t hdr[PWD_BLOB_HEADER_WORDS];
@@ -551,6 +655,14 @@ int decoder_create(const pwd_geometry* geom, const pwd_model_dims* dims, const v
                               ((uint32_t)dims->conv_dilation[2] << 16);
     if (hdr[13] != dil_word)
         return fail(PWD_EBLOB, "blob header word 13 (dilations) is 0x%x, expected 0x%x", hdr[13], dil_word);
+    if (rot) {
+        const uint32_t rot_word = (uint32_t)rot->qk_norm | ((uint32_t)rot->pairs[0] << 8) | ((uint32_t)rot->pairs[1] << 16);
+        uint32_t theta_word;
+        std::memcpy(&theta_word, &rot->theta, 4);
+        if (hdr[14] != rot_word || hdr[15] != theta_word)
+            return fail(PWD_EBLOB, "blob header words 14, 15 (rotary) are 0x%x, 0x%x, expected 0x%x, 0x%x", hdr[14], hdr[15],
+                        rot_word, theta_word);
+    }
     float kappa, eps;
     std::memcpy(&kappa, &hdr[9], 4);
     std::memcpy(&eps, &hdr[10], 4);
@@ -628,7 +740,7 @@ int decoder_create(const pwd_geometry* geom, const pwd_model_dims* dims, const v
             cell_stab[stab_cells[s].first * (d + 1) + stab_cells[s].second] = (int)s;
         std::vector<int> nb;
         std::vector<float> tab;
-        const float* res = w.data() + nf - conv_floats(dims) - res_floats(dims);   // after beta
+        const float* res = w.data() + decoder_blob_floats(geom, dims) - conv_floats(dims) - res_floats(dims);   // after beta
         emb_tables(cells, cell_stab, d, D, w.data(), w.data() + D, res, nb, tab);
         off_emb_nb = put(nb.data(), nb.size() * sizeof(int));
         off_emb_tab = put(tab.data(), tab.size() * sizeof(float));
@@ -639,14 +751,77 @@ int decoder_create(const pwd_geometry* geom, const pwd_model_dims* dims, const v
     size_t off_S0 = 0, off_we = 0, off_Wc = 0, off_bc = 0, off_wo = 0, off_zero = 0;
     size_t off_f32_stream = 0, off_f32_vecs = 0, off_f32_wc = 0, off_f32_conv = 0;
     size_t off_res_stream = 0, off_res_vecs = 0;
-    const bool resident_ok = dims->dtype == PWD_DTYPE_BF16 && !has_conv(dims) && dims->embedder == PWD_EMBED_LINEAR &&
+    const bool resident_ok = !rot && dims->dtype == PWD_DTYPE_BF16 && !has_conv(dims) && dims->embedder == PWD_EMBED_LINEAR &&
                              resident_supported(D, (dec->ntok + 15) / 16, L, dims->mlp_ratio, D / H);
     dec->resident_ok = resident_ok;
     dec->mlp_ratio = dims->mlp_ratio;
     const size_t lf = layer_floats(D, F);
     const float* tail = w.data() + 2 * D + (size_t)L * lf;   // Wc, bc, w_o, b_o, beta
     const bool mx = dims->dtype == PWD_DTYPE_MXFP8;
-    if (dims->dtype != PWD_DTYPE_F32) {
+    struct RotaryOff { size_t wqkv, wo, w1, w2, bqkv, bo, g1, be1, b1, b2, g2, be2, gq, gk; };
+    std::vector<RotaryOff> roff(rot ? L : 0);
+    size_t off_rot_wc = 0;
+    if (rot) {
+        const bool f32 = dims->dtype == PWD_DTYPE_F32, sinusoid = rot->pairs[0] + rot->pairs[1] == 0;
+        // W [K][O] as rows of its outputs, [O][K], in the network's type
+        std::vector<float> tr;
+        std::vector<uint16_t> tb;
+        auto add = [&](const float* W, int K, int O) {
+            for (int o = 0; o < O; ++o)
+                for (int k = 0; k < K; ++k) {
+                    if (f32) tr.push_back(W[(size_t)k * O + o]);
+                    else tb.push_back(to_bf16(W[(size_t)k * O + o]));
+                }
+        };
+        auto flush = [&] {
+            const size_t off = f32 ? put(tr.data(), tr.size() * 4) : put(tb.data(), tb.size() * 2);
+            tr.clear();
+            tb.clear();
+            return off;
+        };
+        std::vector<float> s0((size_t)dec->ntok * D);
+        for (int s = 0; s < dec->ntok; ++s) {
+            pe_of(cells[s].first * (d + 1) + cells[s].second);
+            for (int f = 0; f < D; ++f) s0[(size_t)s * D + f] = (float)((double)b_e[f] + (sinusoid ? pe_row[f] : 0.0));
+        }
+        off_S0 = put(s0.data(), s0.size() * 4);
+        off_we = put(w.data(), (size_t)D * 4);
+        const float* gains = w.data() + nf - rotary_floats(dims, rot);
+        for (int l = 0; l < L; ++l) {
+            const float* q = w.data() + 2 * D + (size_t)l * lf;
+            const float *Wq = q, *bq = Wq + D * D, *Wk = bq + D, *bk = Wk + D * D, *Wv = bk + D, *bv = Wv + D * D;
+            const float *Wo = bv + D, *bo = Wo + D * D, *g1 = bo + D, *be1 = g1 + D, *W1 = be1 + D;
+            const float *b1 = W1 + (size_t)D * F, *W2 = b1 + F, *b2 = W2 + (size_t)F * D, *g2 = b2 + D, *be2 = g2 + D;
+            RotaryOff& o = roff[l];
+            for (const float* m : {Wq, Wk, Wv}) add(m, D, D);
+            o.wqkv = flush();
+            add(Wo, D, D);
+            o.wo = flush();
+            add(W1, D, F);
+            o.w1 = flush();
+            add(W2, F, D);
+            o.w2 = flush();
+            std::vector<float> bqkv(bq, bq + D);
+            bqkv.insert(bqkv.end(), bk, bk + D);
+            bqkv.insert(bqkv.end(), bv, bv + D);
+            o.bqkv = put(bqkv.data(), bqkv.size() * 4);
+            o.bo = put(bo, (size_t)D * 4);
+            o.g1 = put(g1, (size_t)D * 4);
+            o.be1 = put(be1, (size_t)D * 4);
+            o.b1 = put(b1, (size_t)F * 4);
+            o.b2 = put(b2, (size_t)D * 4);
+            o.g2 = put(g2, (size_t)D * 4);
+            o.be2 = put(be2, (size_t)D * 4);
+            if (rot->qk_norm) {
+                o.gq = put(gains + (size_t)l * 2 * dec->dh, (size_t)dec->dh * 4);
+                o.gk = put(gains + ((size_t)l * 2 + 1) * dec->dh, (size_t)dec->dh * 4);
+            }
+        }
+        add(tail, 4 * D, D);
+        off_rot_wc = flush();
+        off_bc = put(tail + 4 * (size_t)D * D, (size_t)D * 4);
+        off_wo = put(tail + 4 * (size_t)D * D + D, (size_t)d * D * 4);
+    } else if (dims->dtype != PWD_DTYPE_F32) {
         const int RT = D / 16;
         std::vector<float> s0((size_t)dec->nbw * RT * 64 * 4, 0.f);
         for (int s = 0; s < dec->ntok; ++s) {
@@ -795,7 +970,32 @@ int decoder_create(const pwd_geometry* geom, const pwd_model_dims* dims, const v
         dec->emb_tab = fptr(off_emb_tab);
     }
     dec->S0 = fptr(off_S0);
-    if (dims->dtype != PWD_DTYPE_F32) {
+    if (rot) {
+        dec->rotary = true;
+        dec->rot = *rot;
+        dec->we = fptr(off_we);
+        dec->bc = fptr(off_bc);
+        dec->wo = fptr(off_wo);
+        dec->rot_wc = base + off_rot_wc;
+        for (const RotaryOff& o : roff)
+            dec->rlayers.push_back({base + o.wqkv, base + o.wo, base + o.w1, base + o.w2, fptr(o.bqkv), fptr(o.bo), fptr(o.g1),
+                                    fptr(o.be1), fptr(o.b1), fptr(o.b2), fptr(o.g2), fptr(o.be2),
+                                    rot->qk_norm ? fptr(o.gq) : nullptr, rot->qk_norm ? fptr(o.gk) : nullptr});
+        // activations and, behind them, every row's (row, column)
+        const size_t ab = RotaryBuffers(dec, dec->max_windows, nullptr).bytes;
+        const size_t rows = (size_t)dec->max_windows * dec->ntok;
+        if ((e = hipMalloc(&dec->rot_act, ab + rows * 8)) != hipSuccess)
+            return cleanup_fail(fail(PWD_ENOMEM, "scratch for %d windows (%zu bytes): %s", dec->max_windows, ab + rows * 8,
+                                     hipGetErrorString(e)));
+        std::vector<int32_t> pos(2 * rows);
+        for (size_t r = 0; r < rows; ++r) {
+            pos[2 * r] = cells[r % dec->ntok].first;
+            pos[2 * r + 1] = cells[r % dec->ntok].second;
+        }
+        dec->rot_pos = reinterpret_cast<const int32_t*>(static_cast<unsigned char*>(dec->rot_act) + ab);
+        e = hipMemcpy(static_cast<unsigned char*>(dec->rot_act) + ab, pos.data(), rows * 8, hipMemcpyHostToDevice);
+        if (e != hipSuccess) return cleanup_fail(fail(PWD_EHIP, "hipMemcpy(positions): %s", hipGetErrorString(e)));
+    } else if (dims->dtype != PWD_DTYPE_F32) {
         dec->we = fptr(off_we);
         dec->Wc = hptr(off_Wc);
         dec->bc = fptr(off_bc);
@@ -873,6 +1073,7 @@ int decoder_destroy(pwd_decoder* dec) {
     (void)hipFree(dec->stream_types);
     (void)hipFree(dec->stream_logits);
     (void)hipFree(dec->stream_bits);
+    (void)hipFree(dec->rot_act);
     for (auto& m : dec->marks) {
         (void)hipEventDestroy(m.begin);
         (void)hipEventDestroy(m.end);
@@ -902,10 +1103,11 @@ struct Activations {
     uint16_t* QKV;
     uint16_t* Y;
     uint16_t* G[2];
+    void* rotary;   // a rotary network's, as RotaryBuffers cuts it up
 };
 
 static Activations handle_activations(const pwd_decoder* dec) {
-    return Activations{dec->X, dec->QKV, dec->Y, {dec->G[0], dec->G[1]}};
+    return Activations{dec->X, dec->QKV, dec->Y, {dec->G[0], dec->G[1]}, dec->rot_act};
 }
 
 // Bytes of X, Q/K/V, Y (and the two G buffers with dilated convolutions) for n_tb token blocks.
@@ -925,6 +1127,139 @@ static int check_batch(const pwd_decoder* dec, const uint32_t* d_meas, const uin
     return PWD_OK;
 }
 
+// Algorithm 1 on the operators: per round the fold, per layer the projections, norm and rotation,
+// attention, LayerNorms and feed-forward, one launch each. The products keep one order of their sums
+// and attention one split of its keys whatever the batch, so a window's result does not depend on it.
+static int decode_rotary(pwd_decoder* dec, const SyndromeIn& in, float* d_logits, uint8_t* d_bits, hipStream_t s,
+                         int readouts, void* buffers) {
+    const RotaryBuffers b(dec, in.nwin, buffers);
+    const bool f32 = dec->dtype == PWD_DTYPE_F32;
+    const int64_t rows = (int64_t)in.nwin * dec->ntok;
+    const int D = dec->D, F = dec->F, es = f32 ? 4 : 2;
+    const void* x_in = f32 ? static_cast<const void*>(b.X) : b.Xb;
+
+    auto linear = [&](const void* x, int64_t m, int k, const void* w, int n, const float* bias, int act, float* residual,
+                      void* y, bool out_f32) {
+        LinearParams p;
+        p.x = x;
+        p.w = w;
+        p.bias = bias;
+        p.residual = residual;
+        p.y = y;
+        p.ldx = p.ldw = k;
+        p.ldr = p.ldy = n;
+        p.m = (int)m;
+        p.n = n;
+        p.k = k;
+        p.act = act;
+        p.f32 = f32;
+        p.out_f32 = out_f32;
+        p.partial = nullptr;
+        p.splits = 1;
+        return launch_linear(p, linear_plan(m, n, k, f32, true), s);
+    };
+    auto norm = [&](const float* gamma, const float* beta) {
+        return launch_row_norm(NormParams{b.X, b.Xb, gamma, beta, rows, D, dec->eps}, s);
+    };
+
+    FoldParams fp;
+    fp.in = in;
+    fp.ntok = dec->ntok;
+    fp.D = D;
+    fp.tok_stab = dec->tok_stab;
+    fp.S0 = dec->S0;
+    fp.we = dec->we;
+    fp.emb_nb = dec->emb_nb;
+    fp.emb_tab = dec->emb_tab;
+    fp.kappa = dec->kappa;
+    fp.X = b.X;
+    fp.Xb = b.Xb;
+
+    RopeParams rp;
+    std::memset(&rp, 0, sizeof rp);
+    const int P = dec->rot.pairs[0] + dec->rot.pairs[1];
+    for (int i = 0; i < 2; ++i) {
+        char* at = static_cast<char*>(b.QKV) + (size_t)i * D * es;
+        rp.t[i] = RopeTensor{at, at, 3 * D, dec->dh, 3 * D, dec->dh, nullptr, dec->H, (((uint64_t)1 << 32) + dec->H - 1) / dec->H};
+    }
+    rp.tokens = rows;
+    rp.pos = dec->rot_pos;
+    rp.axes = 2;
+    rp.pairs = P;
+    rp.dh = dec->dh;
+    rp.eps = dec->rot.norm_eps;
+    rp.norm = dec->rot.qk_norm != 0;
+    int j = 0;
+    for (int a = 0; a < 2; ++a) {
+        for (int i = 0; i < dec->rot.pairs[a]; ++i, ++j)
+            rp.turns[j] = std::pow((double)dec->rot.theta, -(double)i / dec->rot.pairs[a]) / (2.0 * M_PI);
+        rp.axis_end[a] = j;
+    }
+    rp.axis_end[2] = j;
+
+    MhaParams mp;
+    std::memset(&mp, 0, sizeof mp);
+    const char* qkv = static_cast<const char*>(b.QKV);
+    mp.q = qkv;
+    mp.k = qkv + (size_t)D * es;
+    mp.v = qkv + (size_t)2 * D * es;
+    mp.out = b.A;
+    for (int64_t* st : {mp.qs, mp.ks, mp.vs, mp.os}) {
+        const int64_t row = st == mp.os ? D : 3 * D;
+        st[0] = row * dec->ntok;
+        st[1] = row;
+        st[2] = dec->dh;
+    }
+    mp.batch = in.nwin;
+    mp.q_len = mp.k_len = dec->ntok;
+    mp.q_heads = mp.k_heads = dec->H;
+    mp.dh = dec->dh;
+    mp.left = mp.right = dec->rot.window;
+    mp.sinks = dec->rot.window < 0 ? 0 : dec->rot.sinks;
+    mp.scale2 = (float)(1.4426950408889634 / std::sqrt((double)dec->dh));
+    mp.f32 = f32;
+    mp.splits = 1;
+    MhaPlan plan = mha_plan(1, dec->ntok, dec->ntok, dec->H, dec->H, dec->dh, mp.left, mp.right, mp.sinks, f32);
+    plan.splits = 1;
+
+    for (int t = 0; t < dec->W; ++t) {
+        fp.t = t;
+        HIP_OK(timed(dec, PWD_STAGE_EMBED_QKV, s, [&] { return launch_fold(fp, s); }));
+        for (const auto& ly : dec->rlayers) {
+            HIP_OK(timed(dec, PWD_STAGE_POST_QKV, s, [&] {
+                hipError_t e = linear(x_in, rows, D, ly.wqkv, 3 * D, ly.bqkv, PWD_ACT_NONE, nullptr, b.QKV, f32);
+                if (e != hipSuccess || (P == 0 && !rp.norm)) return e;
+                rp.t[0].gain = ly.gq;
+                rp.t[1].gain = ly.gk;
+                return launch_rope(rp, f32, s);
+            }));
+            HIP_OK(timed(dec, PWD_STAGE_ATTENTION, s, [&] { return launch_mha(mp, plan, s); }));
+            HIP_OK(timed(dec, PWD_STAGE_OUT_PROJ, s, [&] {
+                const hipError_t e = linear(b.A, rows, D, ly.wo, D, ly.bo, PWD_ACT_NONE, b.X, b.X, true);
+                return e != hipSuccess ? e : norm(ly.g1, ly.be1);
+            }));
+            HIP_OK(timed(dec, PWD_STAGE_POST, s, [&] {
+                hipError_t e = linear(x_in, rows, D, ly.w1, F, ly.b1, PWD_ACT_RELU, nullptr, b.H, f32);
+                if (e == hipSuccess) e = linear(b.H, rows, F, ly.w2, D, ly.b2, PWD_ACT_NONE, b.X, b.X, true);
+                return e != hipSuccess ? e : norm(ly.g2, ly.be2);
+            }));
+        }
+        if (t < dec->W - readouts) continue;
+        HIP_OK(timed(dec, PWD_STAGE_READOUT, s, [&] {
+            const int64_t cells = (int64_t)in.nwin * dec->d * dec->d;
+            hipError_t e = launch_gather(GatherParams{b.X, b.H, dec->cell_token, in.nwin, dec->d, dec->ntok, D, f32}, s);
+            if (e == hipSuccess)
+                e = linear(b.H, cells, 4 * D, dec->rot_wc, D, dec->bc, PWD_ACT_RELU, nullptr, b.QKV, true);
+            if (e != hipSuccess) return e;
+            const int k = t - (dec->W - readouts);
+            return launch_pool(PoolParams{static_cast<const float*>(b.QKV), dec->wo, in.types, dec->bo_out,
+                                          {dec->beta[0], dec->beta[1], dec->beta[2]}, d_logits + k, d_bits + k, dec->err,
+                                          in.nwin, dec->d, D, readouts}, s);
+        }));
+    }
+    return PWD_OK;
+}
+
 // decode_windows with `readouts` readouts after the last `readouts` rounds (1: the inference
 // branch; distance: the recurrent branch), written to d_logits[win * readouts + k].
 static int decode_impl(pwd_decoder* dec, const uint32_t* d_meas, const uint8_t* d_types, int64_t n,
@@ -937,6 +1272,7 @@ static int decode_impl(pwd_decoder* dec, const uint32_t* d_meas, const uint8_t* 
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     const SyndromeIn in = syndrome_in(dec, d_meas, d_types, n);
 
+    if (dec->rotary) return decode_rotary(dec, in, d_logits, d_bits, s, readouts, act.rotary);
     if (dec->dtype == PWD_DTYPE_F32) {
         F32Params p;
         p.in = in;
@@ -1123,8 +1459,14 @@ int decode_windows_noalloc(pwd_decoder* dec, const uint32_t* d_meas, const uint8
                            float* d_logits, uint8_t* d_bits, void* hip_stream) {
     const int rc = check_batch(dec, d_meas, d_types, n, d_logits, d_bits);
     if (rc != PWD_OK || n == 0) return rc;
-    Activations act{nullptr, nullptr, nullptr, {nullptr, nullptr}};
-    if (dec->dtype != PWD_DTYPE_F32) {
+    Activations act{nullptr, nullptr, nullptr, {nullptr, nullptr}, nullptr};
+    if (dec->rotary) {
+        const size_t need = RotaryBuffers(dec, n, nullptr).bytes;
+        if (need > (size_t)PWD_NOALLOC_SCRATCH_BYTES)
+            return fail(PWD_EBATCH, "%lld windows need %zu bytes of scratch; decode_windows_noalloc has %zu",
+                        (long long)n, need, (size_t)PWD_NOALLOC_SCRATCH_BYTES);
+        act.rotary = dec->static_scratch;
+    } else if (dec->dtype != PWD_DTYPE_F32) {
         // the same token-block rounding as the handle's buffers: every launch's grid fits
         const int64_t gran = tok_block_granule();
         const int64_t n_tb = (n * dec->nbw + gran - 1) / gran * gran;

@@ -40,6 +40,18 @@ class ModelDims(ctypes.Structure):
                 ("embedder", ctypes.c_int32), ("conv_dilation", ctypes.c_int32 * 3)]
 
 
+class RotaryDims(ctypes.Structure):
+    _fields_ = [("pairs", ctypes.c_int32 * 2), ("theta", ctypes.c_float), ("qk_norm", ctypes.c_int32),
+                ("norm_eps", ctypes.c_float), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
+
+
+def rotary_dims(pairs=(0, 0), theta: float = 10000.0, qk_norm: bool = False, norm_eps: float = 1e-6, window: int = -1,
+                sinks: int = 0) -> RotaryDims:
+    """Attention options of a rotary network (decoder_create_rotary): feature pairs of a head turned by the
+    token's lattice row and column, RMS norm of Q and K heads, window of tokens and sinks."""
+    return RotaryDims((ctypes.c_int32 * 2)(*pairs), theta, int(qk_norm), norm_eps, window, sinks)
+
+
 NUM_STAGES = 12
 STAGE_NAMES = ["embed_qkv", "attention", "post_qkv", "post_embed_qkv", "post", "readout", "fp32_window",
                "stream_split", "stream_combine", "out_proj", "dilated_conv", "resident"]
@@ -112,6 +124,10 @@ def bind(lib: ctypes.CDLL) -> ctypes.CDLL:
         "decoder_profile": (ctypes.c_int, [VP, ctypes.c_int]),
         "decoder_schedule": (ctypes.c_int, [VP, ctypes.c_int]),
         "decoder_profile_read": (ctypes.c_int, [VP, P(StageTimes)]),
+        "decoder_rotary_blob_floats": (ctypes.c_size_t, [P(Geometry), P(ModelDims), P(RotaryDims)]),
+        "decoder_validate_rotary": (ctypes.c_int, [P(Geometry), P(ModelDims), P(RotaryDims)]),
+        "decoder_create_rotary": (ctypes.c_int, [P(Geometry), P(ModelDims), P(RotaryDims), ctypes.c_void_p,
+                                                 ctypes.c_size_t, P(VP)]),
         "pwd_linear_workspace": (ctypes.c_size_t, [P(LinearArgs)]),
         "pwd_linear": (ctypes.c_int, [P(LinearArgs), VP]),
         "pwd_rope": (ctypes.c_int, [P(RopeArgs), VP]),
@@ -159,14 +175,18 @@ def pack_dilations(dil) -> int:
 
 
 def make_blob(d: int, W: int, D: int, L: int, H: int, F: int, dtype: int, weights: dict,
-              token_set: int = TOKENS_STABILIZERS) -> bytes:
-    """Serializes a weight dict into the library's blob format (header + fp32 tensors)."""
+              token_set: int = TOKENS_STABILIZERS, rotary: RotaryDims | None = None) -> bytes:
+    """Serializes a weight dict into the library's blob format (header + fp32 tensors). A rotary network's
+    layers hold the norm gains "gq" and "gk" where it norms its queries and keys."""
     kappa = np.float32(weights["kappa"])
     eps = np.float32(weights["eps"])
     hdr = [BLOB_MAGIC, BLOB_VERSION, d, W, D, L, H, F, dtype,
            struct.unpack("<I", struct.pack("<f", kappa))[0],
            struct.unpack("<I", struct.pack("<f", eps))[0], token_set,
            EMBED_RESNET if "res" in weights else EMBED_LINEAR, pack_dilations(weights.get("dilations")), 0, 0]
+    if rotary is not None:
+        hdr[14] = rotary.qk_norm | rotary.pairs[0] << 8 | rotary.pairs[1] << 16
+        hdr[15] = struct.unpack("<I", struct.pack("<f", rotary.theta))[0]
     parts = [weights["w_e"], weights["b_e"]]
     for lw in weights["layers"]:
         parts += [lw[k] for k in ("Wq", "bq", "Wk", "bk", "Wv", "bv", "Wo", "bo", "g1", "be1",
@@ -177,6 +197,9 @@ def make_blob(d: int, W: int, D: int, L: int, H: int, F: int, dtype: int, weight
     if weights.get("dilations"):
         for lw in weights["layers"]:
             parts += [lw["Wd"], lw["bd"]]
+    if rotary is not None and rotary.qk_norm:
+        for lw in weights["layers"]:
+            parts += [lw["gq"], lw["gk"]]
     body = np.concatenate([np.asarray(p, dtype=np.float64).ravel() for p in parts]).astype("<f4")
     return struct.pack("<16I", *hdr) + body.tobytes()
 
@@ -221,7 +244,7 @@ class Decoder:
 
     def __init__(self, d: int, W: int, max_windows: int, D: int, L: int, H: int, mlp_ratio: int,
                  dtype: int, blob: bytes, token_set: int = TOKENS_STABILIZERS, embedder: int = EMBED_LINEAR,
-                 dilations=(0, 0, 0)):
+                 dilations=(0, 0, 0), rotary: RotaryDims | None = None):
         import torch
         # torch's HIP runtime starts first: created the other way round (the library's HIP calls
         # before torch initialises its device), torch then finds no GPU in this process
@@ -234,16 +257,22 @@ class Decoder:
         g, m = geometry(d, W, max_windows), dims(D, L, H, mlp_ratio, dtype, token_set, embedder, dilations)
         h = ctypes.c_void_p()
         buf = ctypes.create_string_buffer(blob, len(blob))
-        _check(lib.decoder_create(ctypes.byref(g), ctypes.byref(m), buf, len(blob), ctypes.byref(h)))
+        if rotary is None:
+            _check(lib.decoder_create(ctypes.byref(g), ctypes.byref(m), buf, len(blob), ctypes.byref(h)))
+        else:
+            _check(lib.decoder_create_rotary(ctypes.byref(g), ctypes.byref(m), ctypes.byref(rotary), buf, len(blob),
+                                             ctypes.byref(h)))
         self._h = h
 
     @classmethod
-    def from_workload(cls, wl, weights: dict, max_windows: int | None = None) -> "Decoder":
+    def from_workload(cls, wl, weights: dict, max_windows: int | None = None,
+                      rotary: RotaryDims | None = None) -> "Decoder":
         ts = TOKENS_GRID if getattr(wl, "grid", False) else TOKENS_STABILIZERS
         emb = EMBED_RESNET if "res" in weights else EMBED_LINEAR
-        blob = make_blob(wl.d, wl.W, wl.D, wl.L, wl.H, wl.F, wl.dtype, weights, ts)
+        blob = make_blob(wl.d, wl.W, wl.D, wl.L, wl.H, wl.F, wl.dtype, weights, ts, rotary)
         dil = tuple(weights["dilations"]) if weights.get("dilations") else (0, 0, 0)
-        return cls(wl.d, wl.W, max_windows or wl.B, wl.D, wl.L, wl.H, wl.mlp_ratio, wl.dtype, blob, ts, emb, dil)
+        return cls(wl.d, wl.W, max_windows or wl.B, wl.D, wl.L, wl.H, wl.mlp_ratio, wl.dtype, blob, ts, emb, dil,
+                   rotary)
 
     def _windows_in(self, meas, types) -> int:
         require(types, "types", ("uint8",), self.device)
