@@ -385,7 +385,7 @@ hipError_t tile(const LinearParams& p, hipStream_t s) {
     const int tm = (p.m + BM - 1) / BM, tn = (p.n + BN - 1) / BN;
     const int smem = 2 * (BM + BN) * 128;
     const void* fn = reinterpret_cast<const void*>(&linear_tile_kernel<F32, BM, BN, WM, WN, DIRECT>);
-    hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
+    hipError_t e = smem > 65536 ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, smem) : hipSuccess;
     if (e != hipSuccess) return e;
     linear_tile_kernel<F32, BM, BN, WM, WN, DIRECT><<<dim3((uint32_t)tm * tn * p.splits), dim3(WM * WN * 64), smem, s>>>(p, tm, tn);
     e = hipGetLastError();

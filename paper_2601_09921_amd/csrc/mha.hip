@@ -387,7 +387,7 @@ hipError_t go(const MhaParams& p, hipStream_t s) {
     const int64_t rows = (int64_t)p.q_len * (p.q_heads / p.k_heads);
     const int row_tiles = (int)((rows + NW * QT * 16 - 1) / (NW * QT * 16));
     const void* fn = reinterpret_cast<const void*>(&mha_kernel<F32, DH, NW, QT>);
-    hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, S::SMEM);
+    hipError_t e = S::SMEM > 65536 ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, S::SMEM) : hipSuccess;
     if (e != hipSuccess) return e;
     mha_kernel<F32, DH, NW, QT><<<dim3((uint32_t)row_tiles * p.k_heads * p.batch * p.splits), dim3(NW * 64), S::SMEM, s>>>(p, row_tiles);
     e = hipGetLastError();

@@ -19,6 +19,21 @@ int element(int dtype) { return dtype == PWD_DTYPE_F32 ? 4 : 2; }
 bool known(int dtype) { return dtype == PWD_DTYPE_F32 || dtype == PWD_DTYPE_BF16; }
 bool aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
+// Does an output of `on` rows lie over an input? Rows that are packed make one range each and must not meet;
+// strided ones may interleave (columns of one buffer), but not start at the same place.
+struct Rows {
+    const void* at;
+    int64_t rows, row, ld;   // elements of a row, from row to row
+    int es;
+};
+bool over(const Rows& o, const Rows& i) {
+    if (!o.at || !i.at || o.rows == 0 || i.rows == 0 || o.row == 0 || i.row == 0) return false;
+    if (o.at == i.at) return true;
+    if ((o.rows > 1 && o.ld != o.row) || (i.rows > 1 && i.ld != i.row)) return false;
+    const char *a = static_cast<const char*>(o.at), *b = static_cast<const char*>(i.at);
+    return a < b + i.rows * i.row * i.es && b < a + o.rows * o.row * o.es;
+}
+
 // Checks of the sizes and options (not the pointers), and the plan they lead to.
 int plan_of(const pwd_linear_args* a, LinearPlan* plan) {
     if (!a) return fail(PWD_EINVAL, "linear: null arguments");
@@ -109,11 +124,16 @@ int rope(const pwd_rope_args* a, bool norm, const float* gain_q, const float* ga
     p.adjacent = a->layout == PWD_ROPE_ADJACENT;
     p.inverse = a->inverse != 0;
     int j = 0;
+    long double f = 0.0L, ratio = 1.0L;
     for (int i = 0; i < 3; ++i) {
-        for (int n = 0; n < a->pairs[i]; ++n, ++j) {
-            const double power = a->frequencies == PWD_ROPE_PER_AXIS ? (double)n / a->pairs[i] : (double)j / (double)total;
-            p.turns[j] = std::pow(a->theta, -power) / (2.0 * M_PI);
+        // the frequencies of a run are a geometric series: one power, and products in 64-bit mantissas, whose
+        // roundings stay below the double's
+        const bool own = a->frequencies == PWD_ROPE_PER_AXIS;
+        if (own || i == 0) {
+            f = 1.0L / (2.0L * M_PIl);
+            ratio = std::pow((long double)a->theta, -1.0L / (own ? (long double)a->pairs[i] : (long double)total));
         }
+        for (int n = 0; n < a->pairs[i]; ++n, ++j, f *= ratio) p.turns[j] = (double)f;
         p.axis_end[i] = j;
     }
     HIP_OK(launch_rope(p, a->dtype == PWD_DTYPE_F32, static_cast<hipStream_t>(stream)));
@@ -177,6 +197,11 @@ int pwd_linear(const pwd_linear_args* a, void* hip_stream) {
         return fail(PWD_EINVAL, "linear: misaligned buffer");
     if (a->d_residual == a->d_y && a->m > 1 && a->ld_residual != a->ld_y)
         return fail(PWD_EINVAL, "linear: the residual in place needs the output's leading dimension");
+    const Rows y{a->d_y, a->m, a->n, a->ld_y, (int)eo};
+    if (over(y, {a->d_x, a->m, a->k, a->ld_x, (int)es}) || over(y, {a->d_w, a->n, a->k, a->ld_w, (int)es}) ||
+        over(y, {a->d_bias, 1, a->n, a->n, 4}) ||
+        (a->d_residual != a->d_y && over(y, {a->d_residual, a->m, a->n, a->ld_residual, (int)eo})))
+        return fail(PWD_EINVAL, "linear: the output lies over an input");
     const size_t need = workspace_of(a, plan);
     if (need && (!a->d_workspace || a->workspace_bytes < need || !aligned(a->d_workspace, 16)))
         return fail(PWD_EINVAL, "linear: needs %zu bytes of workspace, 16-byte aligned", need);
@@ -232,6 +257,8 @@ int pwd_attention(const pwd_attention_args* a, void* hip_stream) {
     for (int i = 0; i < 3; ++i)
         if (len[i] > 1 && a->out_stride[i] < a->head_dim)
             return fail(PWD_EINVAL, "attention: out_stride[%d] = %lld is below head_dim %d", i, (long long)a->out_stride[i], a->head_dim);
+    for (const void* in : {a->d_q, a->d_k, a->d_v})
+        if (in == a->d_out) return fail(PWD_EINVAL, "attention: the output lies over an input");
     const size_t need = workspace_of(a, plan);
     if (need && (!a->d_workspace || a->workspace_bytes < need || !aligned(a->d_workspace, 16)))
         return fail(PWD_EINVAL, "attention: needs %zu bytes of workspace, 16-byte aligned", need);

@@ -381,7 +381,8 @@ class Decoder:
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 ROPE_LAYOUTS = {"half": 0, "adjacent": 1}
 ROPE_FREQUENCIES = {"axis": 0, "shared": 1}
-_OP_DTYPES = {"float32": DTYPE_F32, "bfloat16": DTYPE_BF16}
+_OP_DTYPES = {"torch.float32": DTYPE_F32, "torch.bfloat16": DTYPE_BF16}
+_dtype_codes = {}   # torch.dtype -> PWD_DTYPE_* of those in _OP_DTYPES
 
 
 def _choice(value, table: dict, name: str) -> int:
@@ -390,19 +391,36 @@ def _choice(value, table: dict, name: str) -> int:
     return table[value]
 
 
-def _tensor(t, name: str, dims: int, like=None, dtypes: tuple = tuple(_OP_DTYPES), shape: tuple | None = None):
-    """Checks an operand of an operator: a CUDA tensor of `dims` axes whose last is contiguous, of one of
-    `dtypes`, of `shape` (None in it: any), on the device of `like`. Raises ValueError."""
+def _operand(t, name: str, dims: int) -> tuple[int, int]:
+    """(device, dtype code) of an operator's first operand: a CUDA tensor of `dims` axes, the last contiguous,
+    bfloat16 or float32. Raises ValueError. (Plain attribute reads: these checks are most of what a small
+    call costs on the host.)"""
     if t is None or not getattr(t, "is_cuda", False):
         raise ValueError(f"{name}: must be a CUDA tensor (got {getattr(t, 'device', t)})")
-    if like is not None and t.device.index != like.device.index:
-        raise ValueError(f"{name}: on cuda:{t.device.index}, need cuda:{like.device.index}")
-    if _dtype_names(t) not in dtypes:
-        raise ValueError(f"{name}: dtype {_dtype_names(t)}, need one of {', '.join(dtypes)}")
-    if t.dim() != dims or (shape is not None and any(s is not None and s != n for s, n in zip(shape, t.shape))):
-        need = tuple("any" if s is None else s for s in shape) if shape is not None else f"{dims} axes"
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, need {need}")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    code = _dtype_codes.get(t.dtype)
+    if code is None:
+        if str(t.dtype) not in _OP_DTYPES:
+            raise ValueError(f"{name}: dtype {_dtype_names(t)}, need bfloat16 or float32")
+        code = _dtype_codes[t.dtype] = _OP_DTYPES[str(t.dtype)]
+    if t.dim() != dims:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, need {dims} axes")
+    if t.stride(-1) != 1 and t.size(-1) > 1:
+        raise ValueError(f"{name}: its last axis must be contiguous (strides {tuple(t.stride())})")
+    return t.get_device(), code
+
+
+def _same(t, name: str, dev: int, dtype, shape: tuple):
+    """Checks a further operand: on device `dev`, of torch dtype `dtype` (or a dtype's name), of `shape`, its
+    last axis contiguous. Raises ValueError."""
+    if t is None or not getattr(t, "is_cuda", False):
+        raise ValueError(f"{name}: must be a CUDA tensor (got {getattr(t, 'device', t)})")
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: on cuda:{t.get_device()}, need cuda:{dev}")
+    if t.dtype != dtype and str(t.dtype) != dtype:
+        raise ValueError(f"{name}: dtype {_dtype_names(t)}, need {str(dtype).replace('torch.', '')}")
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, need {tuple(shape)}")
+    if t.stride(-1) != 1 and t.size(-1) > 1:
         raise ValueError(f"{name}: its last axis must be contiguous (strides {tuple(t.stride())})")
 
 
@@ -412,61 +430,43 @@ def _ptr(t):
 
 def _stride(t, axis: int, row: int) -> int:
     """Stride of an axis, that of packed rows where it has one element (torch leaves it arbitrary)."""
-    return t.stride(axis) if t.shape[axis] != 1 else row
+    return t.stride(axis) if t.size(axis) != 1 else row
 
 
-def _span(t) -> tuple[int, int]:
-    """First and past-the-last address of a tensor's elements (none: an empty range)."""
-    if t.numel() == 0:
-        return 0, 0
-    last = sum((n - 1) * s for n, s in zip(t.shape, t.stride()))
-    return t.data_ptr(), t.data_ptr() + (last + 1) * t.element_size()
-
-
-def _apart(out, name: str, *inputs):
-    """Refuses an output that lies over an input as a whole range of addresses (columns of one buffer
-    interleave and are the caller's to keep apart)."""
-    a, b = _span(out)
-    for t in inputs:
-        if t is None:
-            continue
-        c, d = _span(t)
-        dense = all(x.is_contiguous() for x in (out, t))
-        if a < d and c < b and (dense or a == c):
-            raise ValueError(f"{name}: overlaps an input")
-
-
-class _on:
-    """The operators' device and stream: the tensors' device made current, the given stream (which must
-    be of that device) or that device's current one."""
-
-    def __init__(self, t, stream):
-        import torch
-        self.guard = torch.cuda.device(t.device)
-        self.stream = torch.cuda.current_stream(t.device) if stream is None else stream
-        if stream is not None and stream.device.index != t.device.index:
-            raise ValueError(f"stream: of cuda:{stream.device.index}, the tensors are on cuda:{t.device.index}")
-
-    def __enter__(self):
-        self.guard.__enter__()
-        return ctypes.c_void_p(self.stream.cuda_stream)
-
-    def __exit__(self, *exc):
-        return self.guard.__exit__(*exc)
-
-
-def _workspace(need: int, given, like, stream):
-    """The caller's workspace (uint8, at least `need` bytes), or one from torch's allocator for the call's stream."""
-    if given is not None:
-        require(given, "workspace", ("uint8",), like.device.index, min_numel=need)
-        return given
-    if need == 0:
-        return None
+def _call(fn, dev: int, stream, *args):
+    """Runs a library call that ends with a stream argument on device `dev`: on the given stream (which must be
+    of that device) or on that device's current one. Raises PwdError."""
     import torch
     if stream is None:
-        return torch.empty(need, dtype=torch.uint8, device=like.device)
-    with torch.cuda.stream(stream):   # the allocator reuses it in that stream's order
-        return torch.empty(need, dtype=torch.uint8, device=like.device)
+        raw = torch._C._cuda_getCurrentRawStream(dev)
+    else:
+        if stream.device.index != dev:
+            raise ValueError(f"stream: of cuda:{stream.device.index}, the tensors are on cuda:{dev}")
+        raw = stream.cuda_stream
+    if torch.cuda.current_device() == dev:
+        rc = fn(*args, raw)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, raw)
+    if rc != PWD_OK:
+        _check(rc)
+
+
+def _set_workspace(a, need: int, given, dev: int, stream):
+    """Puts the caller's workspace (uint8, at least `need` bytes) into the arguments, or one from torch's
+    allocator, which reuses it in the order of the call's stream. Returns the tensor."""
+    if given is not None:
+        require(given, "workspace", ("uint8",), dev, min_numel=need)
+    elif need:
+        import torch
+        if stream is None:
+            given = torch.empty(need, dtype=torch.uint8, device=f"cuda:{dev}")
+        else:
+            with torch.cuda.stream(stream):
+                given = torch.empty(need, dtype=torch.uint8, device=f"cuda:{dev}")
+    if given is not None:
+        a.d_workspace, a.workspace_bytes = given.data_ptr(), given.numel()
+    return given
 
 
 def linear(x, w, y, bias=None, activation: str = "none", residual=None, workspace=None, stream=None):
@@ -474,81 +474,74 @@ def linear(x, w, y, bias=None, activation: str = "none", residual=None, workspac
     (one row per output feature); bias: float32 [n]; y: bfloat16 or float32 [m][n], residual of y's
     type and shape (y itself allowed). Rows may be strided. activation: none, relu, gelu, gelu_tanh,
     silu. workspace: uint8 cuda tensor of linear_workspace(...) bytes (None: taken from torch)."""
-    a = _linear_args(x, w, y, bias, activation, residual)
-    _apart(y, "y", x, w, bias, residual if residual is not None and residual.data_ptr() != y.data_ptr() else None)
-    lib = load_library()
-    with _on(x, stream) as s:
-        ws = _workspace(lib.pwd_linear_workspace(ctypes.byref(a)), workspace, x, stream)
-        if ws is not None:
-            a.d_workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
-        _check(lib.pwd_linear(ctypes.byref(a), s))
+    a, dev = _linear_args(x, w, y, bias, activation, residual)
+    lib = _lib or load_library()
+    r = ctypes.byref(a)
+    need = lib.pwd_linear_workspace(r)
+    held = _set_workspace(a, need, workspace, dev, stream) if need or workspace is not None else None
+    _call(lib.pwd_linear, dev, stream, r)
+    del held   # not before the call
 
 
-def _linear_args(x, w, y, bias, activation, residual) -> LinearArgs:
-    _tensor(x, "x", 2)
+def _linear_args(x, w, y, bias, activation, residual) -> tuple[LinearArgs, int]:
+    dev, code = _operand(x, "x", 2)
     m, k = x.shape
-    _tensor(w, "w", 2, x, (_dtype_names(x),), (None, k))
-    n = w.shape[0]
-    _tensor(y, "y", 2, x, shape=(m, n))
+    n = w.size(0) if getattr(w, "is_cuda", False) and w.dim() == 2 else 0
+    _same(w, "w", dev, x.dtype, (n, k))
+    _, out = _operand(y, "y", 2)
+    _same(y, "y", dev, y.dtype, (m, n))
     if bias is not None:
-        _tensor(bias, "bias", 1, x, ("float32",), (n,))
+        _same(bias, "bias", dev, "torch.float32", (n,))
+    ld_r = n
     if residual is not None:
-        _tensor(residual, "residual", 2, x, (_dtype_names(y),), (m, n))
-    return LinearArgs(m, n, k, _ptr(x), _stride(x, 0, k), _ptr(w), _stride(w, 0, k), _ptr(bias), _ptr(residual),
-                      _stride(residual, 0, n) if residual is not None else n, _ptr(y), _stride(y, 0, n),
-                      _OP_DTYPES[_dtype_names(x)], _OP_DTYPES[_dtype_names(y)],
-                      _choice(activation, ACTIVATIONS, "activation"))
+        _same(residual, "residual", dev, y.dtype, (m, n))
+        ld_r = _stride(residual, 0, n)
+    return LinearArgs(m, n, k, x.data_ptr(), _stride(x, 0, k), w.data_ptr(), _stride(w, 0, k), _ptr(bias), _ptr(residual), ld_r,
+                      y.data_ptr(), _stride(y, 0, n), code, out, _choice(activation, ACTIVATIONS, "activation")), dev
 
 
 def linear_workspace(x, w, y) -> int:
     """Bytes of workspace that linear takes for these operands."""
-    return load_library().pwd_linear_workspace(ctypes.byref(_linear_args(x, w, y, None, "none", None)))
+    return load_library().pwd_linear_workspace(ctypes.byref(_linear_args(x, w, y, None, "none", None)[0]))
 
 
-def _rope_args(q, k, positions, pairs, theta, layout, frequencies, inverse, q_out, k_out):
+def _rope_args(q, k, positions, pairs, theta, layout, frequencies, inverse, q_out, k_out) -> tuple[RopeArgs, int]:
     ref = q if q is not None else k
     if ref is None:
         raise ValueError("rope: q or k is required")
-    _tensor(ref, "q" if q is not None else "k", 3)
-    tokens, _, dh = ref.shape
-    dt = (_dtype_names(ref),)
-    if k is not None:
-        _tensor(k, "k", 3, ref, dt, (tokens, None, dh))
+    dev, code = _operand(ref, "q" if q is not None else "k", 3)
+    tokens, heads, dh = ref.shape
+    dt = ref.dtype
     if (q_out is not None and q is None) or (k_out is not None and k is None):
         raise ValueError("rope: an output without its input")
-    outs = []
-    for t, o, name in ((q, q_out, "q_out"), (k, k_out, "k_out")):
-        o = t if o is None else o
-        if t is not None:
-            _tensor(o, name, 3, ref, dt, tuple(t.shape))
-            if o.data_ptr() == t.data_ptr() and o.stride() != t.stride() and t.numel():
-                raise ValueError(f"{name}: in place needs the same strides")
-            if o.data_ptr() != t.data_ptr():
-                _apart(o, name, q, k)
-        outs.append(o)
-    pairs = tuple(int(p) for p in pairs)
-    if len(pairs) > 3:
-        raise ValueError(f"pairs: {len(pairs)} axes, need at most 3")
-    if positions is not None and positions.dim() == 1:
-        positions = positions[:, None]
-    if pairs:
-        _tensor(positions, "positions", 2, ref, ("int32",), (tokens, len(pairs)))
+    hq, hk = (heads, 0) if q is not None else (0, heads)
+    if k is not None and q is not None:
+        hk = k.size(1) if getattr(k, "is_cuda", False) and k.dim() == 3 else 0
+        _same(k, "k", dev, dt, (tokens, hk, dh))
+    fields = []
+    for t, n, name in ((q, hq, "q"), (k, hk, "k"), (q_out, hq, "q_out"), (k_out, hk, "k_out")):
+        if t is None and name.endswith("_out"):
+            fields += fields[-6:-3]          # in place
+        elif t is None:
+            fields += [None, 0, 0]
+        else:
+            if name.endswith("_out"):
+                _same(t, name, dev, dt, (tokens, n, dh))
+            fields += [t.data_ptr(), _stride(t, 0, dh * n), _stride(t, 1, dh)]
+    pairs = tuple(pairs)
+    axes = len(pairs)
+    if axes > 3:
+        raise ValueError(f"pairs: {axes} axes, need at most 3")
+    if axes:
+        one = axes == 1 and positions is not None and positions.dim() == 1
+        _same(positions, "positions", dev, "torch.int32", (tokens,) if one else (tokens, axes))
         if not positions.is_contiguous():
             raise ValueError("positions: must be contiguous")
     elif positions is not None:
         raise ValueError("positions: given without pairs")
-    a = RopeArgs(tokens, q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0, dh, _OP_DTYPES[dt[0]])
-    for name, t in (("q", q), ("k", k), ("q_out", outs[0]), ("k_out", outs[1])):
-        if t is not None:
-            setattr(a, f"d_{name}", t.data_ptr())
-            setattr(a, f"{name}_head_stride", _stride(t, 1, dh))
-            setattr(a, f"{name}_token_stride", _stride(t, 0, dh * t.shape[1]))
-    a.d_positions, a.axes = _ptr(positions), len(pairs)
-    a.pairs = (ctypes.c_int32 * 3)(*pairs)
-    a.layout = _choice(layout, ROPE_LAYOUTS, "layout")
-    a.frequencies = _choice(frequencies, ROPE_FREQUENCIES, "frequencies")
-    a.inverse, a.theta = int(bool(inverse)), float(theta)
-    return a, ref
+    return RopeArgs(tokens, hq, hk, dh, code, *fields, _ptr(positions), axes, pairs + (0,) * (3 - axes),
+                    _choice(layout, ROPE_LAYOUTS, "layout"), _choice(frequencies, ROPE_FREQUENCIES, "frequencies"),
+                    1 if inverse else 0, theta), dev
 
 
 def rope(q, k, positions, pairs, theta: float = 10000.0, layout: str = "half", frequencies: str = "axis",
@@ -558,45 +551,41 @@ def rope(q, k, positions, pairs, theta: float = 10000.0, layout: str = "half", f
     q_out / k_out. pairs: feature pairs of each axis. layout: half (pair j is features j and j + P) or
     adjacent (2 j and 2 j + 1); frequencies: axis (theta^(-i / pairs of the axis)) or shared
     (theta^(-j / P)); inverse: undo the rotation."""
-    a, ref = _rope_args(q, k, positions, pairs, theta, layout, frequencies, inverse, q_out, k_out)
-    with _on(ref, stream) as s:
-        _check(load_library().pwd_rope(ctypes.byref(a), s))
+    a, dev = _rope_args(q, k, positions, pairs, theta, layout, frequencies, inverse, q_out, k_out)
+    _call((_lib or load_library()).pwd_rope, dev, stream, ctypes.byref(a))
 
 
 def qk_norm_rope(q, k, gain_q, gain_k, positions, pairs, theta: float = 10000.0, layout: str = "half",
                  frequencies: str = "axis", eps: float = 1e-6, q_out=None, k_out=None, stream=None):
     """RMS norm of every head of q and k (gains float32 [dh], or None), then the rotation of rope, in
     one pass. pairs = () and positions = None: the norm alone."""
-    a, ref = _rope_args(q, k, positions, pairs, theta, layout, frequencies, False, q_out, k_out)
+    a, dev = _rope_args(q, k, positions, pairs, theta, layout, frequencies, False, q_out, k_out)
     for gain, name in ((gain_q, "gain_q"), (gain_k, "gain_k")):
         if gain is not None:
-            _tensor(gain, name, 1, ref, ("float32",), (ref.shape[2],))
-    with _on(ref, stream) as s:
-        _check(load_library().pwd_qk_norm_rope(ctypes.byref(a), ctypes.c_void_p(_ptr(gain_q)),
-                                               ctypes.c_void_p(_ptr(gain_k)), float(eps), s))
+            _same(gain, name, dev, "torch.float32", (a.head_dim,))
+    _call((_lib or load_library()).pwd_qk_norm_rope, dev, stream, ctypes.byref(a), _ptr(gain_q), _ptr(gain_k), eps)
 
 
-def _attention_args(q, k, v, out, window, sinks, scale, q_lengths, k_lengths) -> AttentionArgs:
-    _tensor(q, "q", 4)
+_I64x3 = ctypes.c_int64 * 3
+
+
+def _attention_args(q, k, v, out, window, sinks, scale, q_lengths, k_lengths) -> tuple[AttentionArgs, int]:
+    dev, code = _operand(q, "q", 4)
     b, sq, hq, dh = q.shape
-    dt = (_dtype_names(q),)
-    _tensor(k, "k", 4, q, dt, (b, None, None, dh))
-    _tensor(v, "v", 4, q, dt, tuple(k.shape))
-    _tensor(out, "out", 4, q, dt, tuple(q.shape))
+    dt = q.dtype
+    sk, hk = (k.size(1), k.size(2)) if getattr(k, "is_cuda", False) and k.dim() == 4 else (0, 0)
+    _same(k, "k", dev, dt, (b, sk, hk, dh))
+    _same(v, "v", dev, dt, (b, sk, hk, dh))
+    _same(out, "out", dev, dt, (b, sq, hq, dh))
     for t, name in ((q_lengths, "q_lengths"), (k_lengths, "k_lengths")):
         if t is not None:
-            _tensor(t, name, 1, q, ("int32",), (b,))
-    a = AttentionArgs(b, sq, k.shape[1], hq, k.shape[2], dh, _OP_DTYPES[dt[0]])
-    for name, t in (("q", q), ("k", k), ("v", v), ("out", out)):
-        setattr(a, f"d_{name}", _ptr(t))
-        head = _stride(t, 2, dh)
-        token = _stride(t, 1, dh * t.shape[2])
-        setattr(a, f"{name}_stride", (ctypes.c_int64 * 3)(_stride(t, 0, dh * t.shape[2] * t.shape[1]), token, head))
-    a.d_q_lengths, a.d_k_lengths = _ptr(q_lengths), _ptr(k_lengths)
-    a.window_left, a.window_right = (int(n) for n in window)
-    a.sinks = int(sinks)
-    a.scale = float(scale) if scale is not None else dh ** -0.5
-    return a
+            _same(t, name, dev, "torch.int32", (b,))
+    fields = []
+    for t, n, h in ((q, sq, hq), (k, sk, hk), (v, sk, hk), (out, sq, hq)):
+        fields += [t.data_ptr(), _I64x3(_stride(t, 0, dh * h * n), _stride(t, 1, dh * h), _stride(t, 2, dh))]
+    left, right = window
+    return AttentionArgs(b, sq, sk, hq, hk, dh, code, *fields, _ptr(q_lengths), _ptr(k_lengths), left, right, sinks,
+                         dh ** -0.5 if scale is None and dh else scale or 0.0), dev
 
 
 def attention(q, k, v, out, window=(-1, -1), sinks: int = 0, scale: float | None = None, q_lengths=None,
@@ -608,17 +597,16 @@ def attention(q, k, v, out, window=(-1, -1), sinks: int = 0, scale: float | None
     queries are its last tokens, and output rows past them are left as they are. A query that sees no
     key gives zeros. scale: dh^-0.5 by default. workspace: uint8 cuda tensor of
     attention_workspace(...) bytes (None: taken from torch)."""
-    a = _attention_args(q, k, v, out, window, sinks, scale, q_lengths, k_lengths)
-    _apart(out, "out", q, k, v)
-    lib = load_library()
-    with _on(q, stream) as s:
-        ws = _workspace(lib.pwd_attention_workspace(ctypes.byref(a)), workspace, q, stream)
-        if ws is not None:
-            a.d_workspace, a.workspace_bytes = ws.data_ptr(), ws.numel()
-        _check(lib.pwd_attention(ctypes.byref(a), s))
+    a, dev = _attention_args(q, k, v, out, window, sinks, scale, q_lengths, k_lengths)
+    lib = _lib or load_library()
+    r = ctypes.byref(a)
+    need = lib.pwd_attention_workspace(r)
+    held = _set_workspace(a, need, workspace, dev, stream) if need or workspace is not None else None
+    _call(lib.pwd_attention, dev, stream, r)
+    del held   # not before the call
 
 
 def attention_workspace(q, k, v, out, window=(-1, -1), sinks: int = 0) -> int:
     """Bytes of workspace that attention takes for these operands."""
     return load_library().pwd_attention_workspace(
-        ctypes.byref(_attention_args(q, k, v, out, window, sinks, None, None, None)))
+        ctypes.byref(_attention_args(q, k, v, out, window, sinks, None, None, None)[0]))
