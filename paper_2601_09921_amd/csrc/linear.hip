@@ -49,15 +49,25 @@ PWD_DEV u32x4 load_chunk(const char* p, int left) {
     return v;
 }
 
-PWD_DEV float activate(float v, int act) {
-    switch (act) {
-        case PWD_ACT_RELU: return v < 0.f ? 0.f : v;
-        case PWD_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+// v[i] = act(v[i] + b[i]); one branch for all of them.
+template <int NV>
+PWD_DEV void activate(float* v, const float* b, int act) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) v[i] += b[i];
+    if (act == PWD_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];
+    } else if (act == PWD_ACT_GELU) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] = 0.5f * v[i] * (1.f + erff(v[i] * 0.70710678118654752f));
+    } else if (act == PWD_ACT_GELU_TANH) {
         // 0.5 (1 + tanh u) = 1 / (1 + e^(-2u)); 2 sqrt(2 / pi) log2(e) = 2.3022082
-        case PWD_ACT_GELU_TANH:
-            return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.3022081981f * fmaf(0.044715f * v * v, v, v)));
-        case PWD_ACT_SILU: return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950409f * v));
-        default: return v;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            v[i] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-2.3022081981f * fmaf(0.044715f * v[i] * v[i], v[i], v[i])));
+    } else if (act == PWD_ACT_SILU) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) v[i] *= __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950409f * v[i]));
     }
 }
 
@@ -129,7 +139,7 @@ PWD_DEV void load_bias(const LinearParams& p, int col, float* b) {
 // DIRECT = false (rows that do not start on 16 bytes, or lie more than 4 GB apart within a tile) stages
 // through registers instead, as does the last stage where k ends inside it (zeros past the end).
 template <bool F32, int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void linear_tile_kernel(LinearParams p, int tiles_m, int tiles_n) {
+__global__ __launch_bounds__(WM * WN * 64, 2) void linear_tile_kernel(LinearParams p, int tiles_m, int tiles_n) {
     constexpr int NW = WM * WN, NT = NW * 64;
     constexpr int TT = BM / WM / 16, FT = BN / WN / 16;
     constexpr int ES = F32 ? 4 : 2, CH = 16 / ES, KSTAGE = 128 / ES;
@@ -210,47 +220,69 @@ __global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void linear_tile_
 #pragma unroll
         for (int j = 0; j < CPT; ++j) *reinterpret_cast<u32x4*>(smem + buf * BUF + (tid + j * NT) * 16) = held[j];
     };
-    auto is_direct = [&](int s) { return DIRECT && (s + 1) * KSTAGE <= p.k; };
-
     f32x4 acc[FT][TT];
 #pragma unroll
     for (int f = 0; f < FT; ++f)
 #pragma unroll
         for (int t = 0; t < TT; ++t) acc[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-    if (s_begin < s_end) {
-        if (is_direct(s_begin)) {
-            load_direct(s_begin, 0);
-        } else {
-            load_held(s_begin);
-            store_held(0);
-        }
-    }
-    for (int s = s_begin; s < s_end; ++s) {
-        const int buf = (s - s_begin) & 1;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();   // stage s is whole, and every wavefront is done with the other buffer
-        const bool more = s + 1 < s_end, direct = more && is_direct(s + 1);
-        if (direct) load_direct(s + 1, buf ^ 1);
-        else if (more) load_held(s + 1);
+    auto multiply = [&](int buf) {
         const unsigned char* xt = smem + buf * BUF + (wm * TT * 16 + col) * 128;
         const unsigned char* wt = smem + buf * BUF + (BM + wn * FT * 16 + col) * 128;
+        // one step: the FT products of a token tile; its fragment is read LA steps ahead, the second
+        // k-step's weight fragments one a step during the first, in this order (left to itself the compiler
+        // reads fragments right before their use)
+        constexpr int NS = 2 * TT, LA = NS > 4 ? 3 : 2, A1 = TT > FT ? TT - FT - 1 : 0;
+        const int slot0 = (g ^ (col & 7)) * 16, slot1 = ((4 + g) ^ (col & 7)) * 16;
+        u32x4 a[2][FT], b[LA + 1];
+        auto read_x = [&](int step) {
+            return *reinterpret_cast<const u32x4*>(xt + step % TT * 2048 + (step < TT ? slot0 : slot1));
+        };
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            const int slot = ((ks * 4 + g) ^ (col & 7)) * 16;
-            u32x4 a[FT], b[TT];
+        for (int f = 0; f < FT; ++f) a[0][f] = *reinterpret_cast<const u32x4*>(wt + f * 2048 + slot0);
 #pragma unroll
-            for (int f = 0; f < FT; ++f) a[f] = *reinterpret_cast<const u32x4*>(wt + f * 2048 + slot);
+        for (int i = 0; i < LA; ++i) b[i] = read_x(i);
+        __builtin_amdgcn_sched_group_barrier(0x100, FT + LA, 0);
 #pragma unroll
-            for (int t = 0; t < TT; ++t) b[t] = *reinterpret_cast<const u32x4*>(xt + t * 2048 + slot);
+        for (int step = 0; step < NS; ++step) {
+            const bool more = step + LA < NS, weights = step >= A1 && step < A1 + FT;
+            if (more) b[(step + LA) % (LA + 1)] = read_x(step + LA);
+            if (weights) a[1][step - A1] = *reinterpret_cast<const u32x4*>(wt + (step - A1) * 2048 + slot1);
 #pragma unroll
-            for (int t = 0; t < TT; ++t)
-#pragma unroll
-                for (int f = 0; f < FT; ++f) acc[f][t] = mma<F32>(a[f], b[t], acc[f][t]);
+            for (int f = 0; f < FT; ++f)
+                acc[f][step % TT] = mma<F32>(a[step / TT][f], b[step % (LA + 1)], acc[f][step % TT]);
+            if (more || weights) __builtin_amdgcn_sched_group_barrier(0x100, (more ? 1 : 0) + (weights ? 1 : 0), 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, F32 ? 4 * FT : FT, 0);
         }
-        if (more && !direct) store_held(buf ^ 1);
+    };
+
+    if constexpr (DIRECT) {
+        const int whole = p.k / KSTAGE < s_end ? p.k / KSTAGE : s_end;   // stages that k fills
+        if (s_begin < whole) load_direct(s_begin, 0);
+        for (int s = s_begin; s < whole; ++s) {
+            const int buf = (s - s_begin) & 1;
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();   // stage s is whole, and every wavefront is done with the other buffer
+            if (s + 1 < whole) load_direct(s + 1, buf ^ 1);
+            multiply(buf);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // none is pending here; on every path, by its looks too
+        if (whole < s_end) {
+            __syncthreads();
+            load_held(whole);
+            store_held(0);
+            __syncthreads();
+            multiply(0);
+        }
+    } else {
+        if (s_begin < s_end) load_held(s_begin);
+        for (int s = s_begin; s < s_end; ++s) {
+            const int buf = (s - s_begin) & 1;
+            store_held(buf);   // the last reads of this buffer are a barrier back
+            __syncthreads();
+            if (s + 1 < s_end) load_held(s + 1);
+            multiply(buf);
+        }
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // none is pending here; on every path, by its looks too
 
     const int nc = n0 + wn * FT * 16 + g * 4 * FT;
     if (p.partial) {   // sums of this split; linear_join_kernel adds them up and finishes
@@ -278,7 +310,8 @@ __global__ __launch_bounds__(WM* WN * 64, WM* WN == 8 ? 2 : 2) void linear_tile_
 #pragma unroll
         for (int f = 0; f < FT; ++f)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[4 * f + i] = activate(acc[f][t][i] + bias[4 * f + i], p.act);
+            for (int i = 0; i < 4; ++i) v[4 * f + i] = acc[f][t][i];
+        activate<4 * FT>(v, bias, p.act);
         if (row < p.m) finish<4 * FT>(p, row, nc, v);
     }
 }
@@ -303,8 +336,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
                 if (c + i < p.n) v[i] += q[i];
         }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = activate(v[i] + b[i], p.act);
+    activate<4>(v, b, p.act);
     finish<4>(p, row, c, v);
 }
 
@@ -369,7 +401,8 @@ __global__ __launch_bounds__(NW * 64) void linear_rows_kernel(LinearParams p) {
         float v[4], b[4];
         load_bias<4>(p, c, b);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = activate(s[e] + b[e], p.act);
+        for (int e = 0; e < 4; ++e) v[e] = s[e];
+        activate<4>(v, b, p.act);
         finish<4>(p, row, c, v);
     }
 }
