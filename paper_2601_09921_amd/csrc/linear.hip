@@ -225,7 +225,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void linear_tile_kernel(LinearPara
     for (int f = 0; f < FT; ++f)
 #pragma unroll
         for (int t = 0; t < TT; ++t) acc[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto multiply = [&](int buf) {
+    auto multiply = [&](int buf, auto load) {   // load(): what is to be under way meanwhile
         const unsigned char* xt = smem + buf * BUF + (wm * TT * 16 + col) * 128;
         const unsigned char* wt = smem + buf * BUF + (BM + wn * FT * 16 + col) * 128;
         // one step: the FT products of a token tile; its fragment is read LA steps ahead, the second
@@ -242,6 +242,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void linear_tile_kernel(LinearPara
 #pragma unroll
         for (int i = 0; i < LA; ++i) b[i] = read_x(i);
         __builtin_amdgcn_sched_group_barrier(0x100, FT + LA, 0);
+        load();
 #pragma unroll
         for (int step = 0; step < NS; ++step) {
             const bool more = step + LA < NS, weights = step >= A1 && step < A1 + FT;
@@ -250,28 +251,33 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void linear_tile_kernel(LinearPara
 #pragma unroll
             for (int f = 0; f < FT; ++f)
                 acc[f][step % TT] = mma<F32>(a[step / TT][f], b[step % (LA + 1)], acc[f][step % TT]);
-            if (more || weights) __builtin_amdgcn_sched_group_barrier(0x100, (more ? 1 : 0) + (weights ? 1 : 0), 0);
+            if (more && weights) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            else if (more || weights) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x008, F32 ? 4 * FT : FT, 0);
         }
     };
 
     if constexpr (DIRECT) {
         const int whole = p.k / KSTAGE < s_end ? p.k / KSTAGE : s_end;   // stages that k fills
+        auto nothing = [] {};
         if (s_begin < whole) load_direct(s_begin, 0);
-        for (int s = s_begin; s < whole; ++s) {
+        for (int s = s_begin; s + 1 < whole; ++s) {
             const int buf = (s - s_begin) & 1;
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();   // stage s is whole, and every wavefront is done with the other buffer
-            if (s + 1 < whole) load_direct(s + 1, buf ^ 1);
-            multiply(buf);
+            multiply(buf, [&] { load_direct(s + 1, buf ^ 1); });
         }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // none is pending here; on every path, by its looks too
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (s_begin < whole) {
+            __syncthreads();
+            multiply((whole - 1 - s_begin) & 1, nothing);
+        }
         if (whole < s_end) {
             __syncthreads();
             load_held(whole);
             store_held(0);
             __syncthreads();
-            multiply(0);
+            multiply(0, nothing);
         }
     } else {
         if (s_begin < s_end) load_held(s_begin);
@@ -280,7 +286,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void linear_tile_kernel(LinearPara
             store_held(buf);   // the last reads of this buffer are a barrier back
             __syncthreads();
             if (s + 1 < s_end) load_held(s + 1);
-            multiply(buf);
+            multiply(buf, [] {});
         }
     }
 
