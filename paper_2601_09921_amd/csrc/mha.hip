@@ -33,7 +33,8 @@ template <bool F32, int DH, int NW, int QT>
 struct Shape {
     static constexpr int ES = F32 ? 4 : 2, CH = 16 / ES;   // element bytes, elements of a 16-byte chunk
     // keys of a tile: a single wavefront stages it all, which at 256 features fits its registers by half
-    static constexpr int KT = (F32 ? 32 : 64) / (NW == 1 && DH == 256 ? 2 : 1);
+    // (four wavefronts: 128 keys at small heads, where a tile's products are few beside its barrier)
+    static constexpr int KT = (F32 ? 32 : 64) * (NW == 1 && DH == 256 ? 1 : NW > 1 && DH == 32 && !F32 ? 4 : 2) / 2;
     static constexpr int CK = DH / CH;                     // chunks of a row
     static constexpr int KSQ = CK / 4;                     // k-steps of a score: four chunks
     static constexpr int KB = KT * DH * ES, VB = KB;       // bytes of a tile of K, of V
@@ -56,11 +57,11 @@ PWD_DEV int slot_of(int r, int c) {
 template <int KT>
 PWD_DEV int vt_slot(int f, int c) {
     constexpr int N = KT / 8;
-    return f * N + (c ^ ((N == 8 ? f ^ (f >> 3) : (f >> 1) ^ (f >> 3)) & (N - 1)));
+    return f * N + (c ^ ((N >= 8 ? f ^ (f >> 3) : (f >> 1) ^ (f >> 3)) & (N < 8 ? N - 1 : 7)));
 }
 
 template <bool F32, int DH, int NW, int QT>
-__global__ __launch_bounds__(NW * 64) void mha_kernel(MhaParams p, int row_tiles) {
+__global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? 2 : 1) void mha_kernel(MhaParams p, int row_tiles) {
     using S = Shape<F32, DH, NW, QT>;
     constexpr int ES = S::ES, CH = S::CH, KT = S::KT, CK = S::CK, KSQ = S::KSQ, NT = S::NT;
     constexpr int ST = KT / 16;          // 16-key tiles
@@ -178,11 +179,18 @@ __global__ __launch_bounds__(NW * 64) void mha_kernel(MhaParams p, int row_tiles
     };
 
     f32x4 acc[OT][QT];
-    float m[QT], l[QT];   // running maximum of the scaled scores (a lower bound within 2^8), this lane's part of the sum
+    // running maximum of the scores (a lower bound, within 2^8 of the weights), and the weights' sum: bf16 on the
+    // matrix core (a row of ones times the weights), fp32 this lane's part
+    float m[QT];
+    f32x4 l[QT];
+    bf16x8 ones;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ones[i] = (__bf16)1.f;
+    const float grow_by = 8.f / p.scale2;
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         m[t] = -__builtin_inff();
-        l[t] = 0.f;
+        l[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int o = 0; o < OT; ++o) acc[o][t] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -217,41 +225,41 @@ __global__ __launch_bounds__(NW * 64) void mha_kernel(MhaParams p, int row_tiles
                 }
             }
         }
-        // scale; hide keys where the tile is not in sight of every row
-        const bool all = key0 + KT <= hi_all && (key0 >= lo_all || key0 + KT <= p.sinks);
-        float top[QT];
+        // hide keys where the tile is not in sight of every row
+        if (!(key0 + KT <= hi_all && (key0 >= lo_all || key0 + KT <= p.sinks))) {
 #pragma unroll
-        for (int t = 0; t < QT; ++t) {
-            top[t] = -__builtin_inff();
+            for (int t = 0; t < QT; ++t)
 #pragma unroll
-            for (int kt = 0; kt < ST; ++kt)
+                for (int kt = 0; kt < ST; ++kt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float v = s[kt][t][i] * p.scale2;
-                    if (!all) {
+                    for (int i = 0; i < 4; ++i) {
                         const int key = key0 + kt * 16 + 4 * g + i;
-                        v = key < hi[t] && (key >= lo[t] || key < p.sinks) ? v : -__builtin_inff();
+                        if (!(key < hi[t] && (key >= lo[t] || key < p.sinks))) s[kt][t][i] = -__builtin_inff();
                     }
-                    s[kt][t][i] = v;
-                    top[t] = fmaxf(top[t], v);
-                }
         }
-        // the maximum moves only where some row's scores would exceed it by more than 2^8: the weights
-        // then stay below 2^8 and the sums far inside fp32, and most tiles leave the output as it is
+        // the maximum moves only where some row's weights would exceed 2^8: the sums stay far inside fp32, and
+        // most tiles leave the output as it is
+        float top[QT];
         bool grow = false;
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
+            top[t] = s[0][t][0];
+#pragma unroll
+            for (int kt = 0; kt < ST; ++kt)
+#pragma unroll
+                for (int i = kt == 0; i < 4; ++i) top[t] = fmaxf(top[t], s[kt][t][i]);
             top[t] = group_max(top[t]);
-            grow = grow || top[t] > m[t] + 8.f;
+            grow = grow || top[t] > m[t] + grow_by;
         }
         if (__builtin_amdgcn_ballot_w64(grow) != 0) {
 #pragma unroll
             for (int t = 0; t < QT; ++t) {
                 const float mn = fmaxf(m[t], top[t]);
                 // a row that has seen no key yet (mn = -inf) keeps its zeros
-                const float c = mn > m[t] ? __builtin_amdgcn_exp2f(m[t] - mn) : 1.f;
+                const float c = mn > m[t] ? __builtin_amdgcn_exp2f((m[t] - mn) * p.scale2) : 1.f;
                 m[t] = mn;
-                l[t] *= c;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) l[t][i] *= c;
 #pragma unroll
                 for (int o = 0; o < OT; ++o)
 #pragma unroll
@@ -260,14 +268,13 @@ __global__ __launch_bounds__(NW * 64) void mha_kernel(MhaParams p, int row_tiles
         }
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const float mt = m[t] == -__builtin_inff() ? 0.f : m[t];
+            const float mt = m[t] == -__builtin_inff() ? 0.f : -m[t] * p.scale2;
 #pragma unroll
             for (int kt = 0; kt < ST; ++kt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float w = __builtin_amdgcn_exp2f(s[kt][t][i] - mt);
-                    s[kt][t][i] = w;
-                    l[t] += w;
+                    s[kt][t][i] = __builtin_amdgcn_exp2f(fmaf(s[kt][t][i], p.scale2, mt));
+                    if constexpr (F32) l[t][0] += s[kt][t][i];
                 }
         }
         if constexpr (F32) {
@@ -290,7 +297,10 @@ __global__ __launch_bounds__(NW * 64) void mha_kernel(MhaParams p, int row_tiles
             for (int kp = 0; kp < ST / 2; ++kp) {
                 bf16x8 w[QT];
 #pragma unroll
-                for (int t = 0; t < QT; ++t) w[t] = pack_b(s[2 * kp][t], s[2 * kp + 1][t]);
+                for (int t = 0; t < QT; ++t) {
+                    w[t] = pack_b(s[2 * kp][t], s[2 * kp + 1][t]);
+                    l[t] = mfma16x16x32(ones, w[t], l[t]);
+                }
 #pragma unroll
                 for (int o = 0; o < OT; ++o) {
                     const u32x4 a = *reinterpret_cast<const u32x4*>(vt + vt_slot<KT>(o * 16 + col, kp * 4 + g) * 16);
@@ -304,7 +314,7 @@ __global__ __launch_bounds__(NW * 64) void mha_kernel(MhaParams p, int row_tiles
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
         const int64_t r = row0 + (wave * QT + t) * 16 + col;
-        const float sum = group_sum(l[t]);
+        const float sum = F32 ? group_sum(l[t][0]) : l[t][0];
         if (r >= row_end) continue;
         const int64_t tok = r / G;
         const int head = hk * G + (int)(r % G);
@@ -319,7 +329,7 @@ __global__ __launch_bounds__(NW * 64) void mha_kernel(MhaParams p, int row_tiles
                     if (f * 16 + 4 * g + i < p.dh) o[f * 16 + 4 * g + i] = acc[f][t][i];
             if (g == 0) {
                 float* ml = p.partial + (int64_t)p.splits * all_rows * p.dh + ((int64_t)split * all_rows + row) * 2;
-                ml[0] = m[t];
+                ml[0] = m[t] * p.scale2;
                 ml[1] = sum;
             }
         } else {
@@ -431,7 +441,7 @@ MhaPlan mha_plan(int64_t batch, int64_t q_len, int64_t k_len, int q_heads, int k
     }
     const int64_t tiles = (keys + KT - 1) / KT;
     int64_t splits = 1;
-    const int64_t want = pl.waves == 1 ? 1024 : 512;
+    const int64_t want = pl.waves == 1 ? 4096 : 512;
     if (wgs < want / 2) splits = want / (wgs > 0 ? wgs : 1);
     if (splits > tiles / 4) splits = tiles / 4;
     if (splits > 128) splits = 128;
