@@ -72,9 +72,13 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? 2 : 1) void mha_kern
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
 
     // workgroup -> (sequence, key head, rows, split): the row tiles of one key head to one XCD (they read
-    // the same keys), the last rows first (under a causal mask they have the most to do)
-    const int total = gridDim.x, per = total / 8, rest = total % 8, xcd = blockIdx.x % 8;
-    int id = xcd * per + (xcd < rest ? xcd : rest) + blockIdx.x / 8;
+    // the same keys), the last rows first (under a causal mask they have the most to do). With one row tile
+    // nothing is shared, and sequences of any lengths are spread over all XCDs.
+    int id = blockIdx.x;
+    if (row_tiles > 1) {
+        const int per = gridDim.x / 8, rest = gridDim.x % 8, xcd = id % 8;
+        id = xcd * per + (xcd < rest ? xcd : rest) + id / 8;
+    }
     const int split = id % p.splits;
     id /= p.splits;
     const int rt = row_tiles - 1 - id % row_tiles;
@@ -355,40 +359,52 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? 2 : 1) void mha_kern
     }
 }
 
-// Joins the splits of each row in their order: 64 lanes a row.
-template <bool F32>
+// Joins the splits of each row: a workgroup a row. The splits' factors first (one a thread, the maximum and
+// the sum through LDS), then, feature by feature, groups of threads add every so many splits and one of
+// them the groups' sums: loads that do not wait for each other, and one order of the additions.
+constexpr int MAX_SPLITS = 128;
+template <bool F32, int DH>
 __global__ __launch_bounds__(256) void mha_join_kernel(MhaParams p) {
-    const int64_t all_rows = (int64_t)p.batch * p.q_len * p.q_heads;
-    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 64;
-    if (row >= all_rows) return;
-    const int lane = threadIdx.x & 63;
-    const int head = (int)(row % p.q_heads);
+    constexpr int GROUPS = 256 / DH;
+    __shared__ float ms[MAX_SPLITS], factor[MAX_SPLITS], sums[MAX_SPLITS], part[256];
+    const int64_t all_rows = (int64_t)p.batch * p.q_len * p.q_heads, row = blockIdx.x;
+    const int tid = threadIdx.x, head = (int)(row % p.q_heads);
     const int64_t tok = row / p.q_heads % p.q_len;
     const int b = (int)(row / p.q_heads / p.q_len);
     if (p.q_lengths && tok >= p.q_lengths[b]) return;   // a row of padding stays as it is
     const float* ml = p.partial + (int64_t)p.splits * all_rows * p.dh + row * 2;
-    float m = -__builtin_inff();
-    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, ml[s * all_rows * 2]);
-    const float mt = m == -__builtin_inff() ? 0.f : m;
-    float sum = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < p.splits; ++s) {
-        const float part = ml[s * all_rows * 2 + 1];
-        if (part == 0.f) continue;   // saw no key
-        const float w = __builtin_amdgcn_exp2f(ml[s * all_rows * 2] - mt);
-        sum = fmaf(part, w, sum);
-        const float* o = p.partial + (s * all_rows + row) * p.dh;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (lane + 64 * j < p.dh) v[j] = fmaf(o[lane + 64 * j], w, v[j]);
+    if (tid < p.splits) {
+        ms[tid] = ml[tid * all_rows * 2];
+        sums[tid] = ml[tid * all_rows * 2 + 1];
     }
-    const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;
-    const int64_t at = b * p.os[0] + tok * p.os[1] + head * p.os[2];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (lane + 64 * j < p.dh) {
-            if constexpr (F32) static_cast<float*>(p.out)[at + lane + 64 * j] = v[j] * inv;
-            else static_cast<__bf16*>(p.out)[at + lane + 64 * j] = (__bf16)(v[j] * inv);
+    __syncthreads();
+    float m = -__builtin_inff();
+    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, ms[s]);
+    // a split that saw no key has a sum of 0 and nothing that counts
+    if (tid < p.splits) factor[tid] = sums[tid] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[tid] - m);
+    __syncthreads();
+    float sum = 0.f;
+    for (int s = 0; s < p.splits; ++s) sum = fmaf(sums[s], factor[s], sum);
+    const int f = tid % DH, group = tid / DH;
+    float v = 0.f;
+    if (f < p.dh) {
+        const float* o = p.partial + row * p.dh + f;
+#pragma unroll 8
+        for (int s = group; s < p.splits; s += GROUPS) {
+            const float c = factor[s], x = o[s * all_rows * p.dh];
+            v = sums[s] == 0.f ? v : fmaf(x, c, v);
         }
+    }
+    part[tid] = v;
+    __syncthreads();
+    if (group == 0 && f < p.dh) {
+#pragma unroll
+        for (int k = 1; k < GROUPS; ++k) v += part[k * DH + f];
+        v *= sum > 0.f || sum != sum ? 1.f / sum : 0.f;
+        const int64_t at = b * p.os[0] + tok * p.os[1] + head * p.os[2] + f;
+        if constexpr (F32) static_cast<float*>(p.out)[at] = v;
+        else static_cast<__bf16*>(p.out)[at] = (__bf16)v;
+    }
 }
 
 template <bool F32, int DH, int NW, int QT>
@@ -403,7 +419,7 @@ hipError_t go(const MhaParams& p, hipStream_t s) {
     e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t all_rows = (int64_t)p.batch * p.q_len * p.q_heads;
-    mha_join_kernel<F32><<<dim3((uint32_t)((all_rows + 3) / 4)), dim3(256), 0, s>>>(p);
+    mha_join_kernel<F32, DH><<<dim3((uint32_t)all_rows), dim3(256), 0, s>>>(p);
     return hipGetLastError();
 }
 
@@ -441,10 +457,10 @@ MhaPlan mha_plan(int64_t batch, int64_t q_len, int64_t k_len, int q_heads, int k
     }
     const int64_t tiles = (keys + KT - 1) / KT;
     int64_t splits = 1;
-    const int64_t want = pl.waves == 1 ? 4096 : 512;
+    const int64_t want = pl.waves == 1 ? 2048 : 512;
     if (wgs < want / 2) splits = want / (wgs > 0 ? wgs : 1);
     if (splits > tiles / 4) splits = tiles / 4;
-    if (splits > 128) splits = 128;
+    if (splits > MAX_SPLITS) splits = MAX_SPLITS;
     pl.splits = splits < 1 ? 1 : (int)splits;
     return pl;
 }
