@@ -6,6 +6,9 @@
 // (i = l % 16, g = l / 16) holding row or column i and chunk g of a k-step of four chunks. For bf16
 // that is one v_mfma_f32_16x16x32_bf16; for fp32 element e of the four chunks is the k-step of
 // v_mfma_f32_16x16x4_f32 number e (any order of k serves, as long as both operands share it).
+#include <algorithm>
+#include <cmath>
+
 #include "common.h"
 #include "ops.h"
 #include "../../include/pwdec.h"
@@ -445,25 +448,47 @@ hipError_t tiles(const LinearParams& p, int kernel, hipStream_t s) {
 
 }  // namespace
 
+// The kernel and the splits along k. Up to 64 rows the weights' bytes count, and the kernel for few rows
+// takes them. Beyond, the cheapest of the tiles and splits by this estimate of the product's time in
+// microseconds: a CU runs `most` workgroups of a tile side by side; one of them takes `alone` per stage
+// of k by its loads' latency, and all of them at least `each` apiece by LDS and the matrix core (256: 1.6
+// measured at 16384 x 8192 x 4096; 64: 0.45 alone at 128 x 4096 x 4096). Splits add a launch and the partial
+// sums' way to memory and back.
 LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, bool f32, bool in_order) {
     if (!in_order && m <= 64) return {m <= 16 ? LIN_ROWS16 : m <= 32 ? LIN_ROWS32 : LIN_ROWS64, 1};
-    auto tiles_of = [&](int64_t t) { return ((m + t - 1) / t) * ((n + t - 1) / t); };
-    if (tiles_of(256) >= 192) return {LIN_TILE256, 1};
-    if (tiles_of(128) >= 192) return {LIN_TILE128, 1};
-    return {LIN_TILE64, 1};
+    struct Tile { int kernel, edge, most; double each; };
+    static constexpr Tile tiles[] = {{LIN_TILE256, 256, 1, 1.6}, {LIN_TILE128, 128, 2, 0.5}, {LIN_TILE64, 64, 4, 0.22}};
+    const double stages = std::ceil((double)k / (f32 ? 32 : 64)), alone = 0.45, slow = f32 ? 3.5 : 1.0;
+    LinearPlan best = {LIN_TILE64, 1};
+    double least = 1e300;
+    for (const Tile& t : tiles) {
+        const double count = std::ceil((double)m / t.edge) * std::ceil((double)n / t.edge);
+        for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
+            if (splits > 1 && (in_order || stages < 4 * splits || count * splits > 1024)) break;
+            const double groups = count * splits, rounds = std::ceil(groups / (256.0 * t.most));
+            const double beside = std::min((double)t.most, std::ceil(groups / 256.0));
+            double time = rounds * std::ceil(stages / splits) * std::max(alone, beside * t.each * slow);
+            if (splits > 1) time += 4.0 + 8.0 * (double)m * (double)n * splits / 4e6;
+            if (time < least) {
+                least = time;
+                best = {t.kernel, splits};
+            }
+        }
+    }
+    return best;
 }
 
 int64_t linear_threads(const LinearPlan& plan, int64_t m, int64_t n) {
     const int64_t t = plan.kernel == LIN_TILE256 ? 256 : plan.kernel == LIN_TILE128 ? 128 : 64;
-    if (plan.kernel < LIN_TILE64) return (n + 15) / 16 * 512;
+    if (plan.kernel < LIN_TILE64) return (n + 15) / 16 * 1024;
     return (m + t - 1) / t * ((n + t - 1) / t) * plan.splits * (t == 256 ? 512 : 256);
 }
 
 hipError_t launch_linear(const LinearParams& p, const LinearPlan& plan, hipStream_t s) {
     switch (plan.kernel) {
-        case LIN_ROWS16: return p.f32 ? rows<true, 1, 8>(p, s) : rows<false, 1, 8>(p, s);
-        case LIN_ROWS32: return p.f32 ? rows<true, 2, 8>(p, s) : rows<false, 2, 8>(p, s);
-        case LIN_ROWS64: return p.f32 ? rows<true, 4, 8>(p, s) : rows<false, 4, 8>(p, s);
+        case LIN_ROWS16: return p.f32 ? rows<true, 1, 16>(p, s) : rows<false, 1, 16>(p, s);
+        case LIN_ROWS32: return p.f32 ? rows<true, 2, 16>(p, s) : rows<false, 2, 16>(p, s);
+        case LIN_ROWS64: return p.f32 ? rows<true, 4, 16>(p, s) : rows<false, 4, 16>(p, s);
         default: break;
     }
     // direct loads copy 16-byte chunks from 32-bit offsets within a tile of up to 256 rows

@@ -359,32 +359,44 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? 2 : 1) void mha_kern
     }
 }
 
-// Joins the splits of each row: a workgroup a row. The splits' factors first (one a thread, the maximum and
-// the sum through LDS), then, feature by feature, groups of threads add every so many splits and one of
-// them the groups' sums: loads that do not wait for each other, and one order of the additions.
+// Joins the splits of each row: a workgroup a row. The first wavefront works out the splits' factors, two a
+// lane; then, feature by feature, groups of threads add every so many splits and one of them the groups'
+// sums: loads that do not wait for each other, and one order of the additions. (128 splits of 32 rows: 25 us
+// with 256 threads that looped over the factors.)
 constexpr int MAX_SPLITS = 128;
 template <bool F32, int DH>
-__global__ __launch_bounds__(256) void mha_join_kernel(MhaParams p) {
-    constexpr int GROUPS = 256 / DH;
-    __shared__ float ms[MAX_SPLITS], factor[MAX_SPLITS], sums[MAX_SPLITS], part[256];
+__global__ __launch_bounds__(1024) void mha_join_kernel(MhaParams p) {
+    constexpr int GROUPS = 1024 / DH;
+    __shared__ float factor[MAX_SPLITS], part[1024], total;
     const int64_t all_rows = (int64_t)p.batch * p.q_len * p.q_heads, row = blockIdx.x;
     const int tid = threadIdx.x, head = (int)(row % p.q_heads);
     const int64_t tok = row / p.q_heads % p.q_len;
     const int b = (int)(row / p.q_heads / p.q_len);
     if (p.q_lengths && tok >= p.q_lengths[b]) return;   // a row of padding stays as it is
-    const float* ml = p.partial + (int64_t)p.splits * all_rows * p.dh + row * 2;
-    if (tid < p.splits) {
-        ms[tid] = ml[tid * all_rows * 2];
-        sums[tid] = ml[tid * all_rows * 2 + 1];
+    if (tid < 64) {
+        const float* ml = p.partial + (int64_t)p.splits * all_rows * p.dh + row * 2;
+        float m[2], l[2], top = -__builtin_inff(), sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int s = tid + 64 * j;
+            m[j] = s < p.splits ? ml[s * all_rows * 2] : -__builtin_inff();
+            l[j] = s < p.splits ? ml[s * all_rows * 2 + 1] : 0.f;
+            top = fmaxf(top, m[j]);
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            // a split that saw no key has a sum of 0 and nothing that counts
+            const float c = l[j] == 0.f ? 0.f : __builtin_amdgcn_exp2f(m[j] - top);
+            factor[tid + 64 * j] = c;
+            sum = l[j] == 0.f ? sum : fmaf(l[j], c, sum);
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        if (tid == 0) total = sum;
     }
     __syncthreads();
-    float m = -__builtin_inff();
-    for (int s = 0; s < p.splits; ++s) m = fmaxf(m, ms[s]);
-    // a split that saw no key has a sum of 0 and nothing that counts
-    if (tid < p.splits) factor[tid] = sums[tid] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[tid] - m);
-    __syncthreads();
-    float sum = 0.f;
-    for (int s = 0; s < p.splits; ++s) sum = fmaf(sums[s], factor[s], sum);
     const int f = tid % DH, group = tid / DH;
     float v = 0.f;
     if (f < p.dh) {
@@ -392,7 +404,7 @@ __global__ __launch_bounds__(256) void mha_join_kernel(MhaParams p) {
 #pragma unroll 8
         for (int s = group; s < p.splits; s += GROUPS) {
             const float c = factor[s], x = o[s * all_rows * p.dh];
-            v = sums[s] == 0.f ? v : fmaf(x, c, v);
+            v = c == 0.f ? v : fmaf(x, c, v);
         }
     }
     part[tid] = v;
@@ -400,6 +412,7 @@ __global__ __launch_bounds__(256) void mha_join_kernel(MhaParams p) {
     if (group == 0 && f < p.dh) {
 #pragma unroll
         for (int k = 1; k < GROUPS; ++k) v += part[k * DH + f];
+        const float sum = total;
         v *= sum > 0.f || sum != sum ? 1.f / sum : 0.f;
         const int64_t at = b * p.os[0] + tok * p.os[1] + head * p.os[2] + f;
         if constexpr (F32) static_cast<float*>(p.out)[at] = v;
@@ -419,7 +432,7 @@ hipError_t go(const MhaParams& p, hipStream_t s) {
     e = hipGetLastError();
     if (e != hipSuccess || p.splits == 1) return e;
     const int64_t all_rows = (int64_t)p.batch * p.q_len * p.q_heads;
-    mha_join_kernel<F32, DH><<<dim3((uint32_t)all_rows), dim3(256), 0, s>>>(p);
+    mha_join_kernel<F32, DH><<<dim3((uint32_t)all_rows), dim3(1024), 0, s>>>(p);
     return hipGetLastError();
 }
 

@@ -162,7 +162,8 @@ int plan_of(const pwd_attention_args* a, MhaPlan* plan) {
     const int64_t per = plan->waves * plan->tiles * 16;
     const double rows = (double)a->q_len * (a->q_heads / a->k_heads);
     const double groups = std::ceil(rows / per) * a->k_heads * (double)a->batch * plan->splits;
-    if (groups * plan->waves * 64 >= (double)THREADS_MAX)
+    const double join = plan->splits > 1 ? (double)a->batch * a->q_len * a->q_heads * 1024.0 : 0.0;
+    if (groups * plan->waves * 64 >= (double)THREADS_MAX || join >= (double)THREADS_MAX)
         return fail(PWD_EUNSUPPORTED, "attention: %lld x %lld x %d query rows are too many for one launch",
                     (long long)a->batch, (long long)a->q_len, a->q_heads);
     return PWD_OK;
