@@ -351,16 +351,20 @@ __global__ __launch_bounds__(256) void linear_join_kernel(LinearParams p) {
 
 // ---- few rows -----------------------------------------------------------------------------
 //
-// Up to 16 TB rows: the weights' bytes are what counts, each read once, so they go from memory
-// straight to the registers the matrix core reads, without LDS. A workgroup owns 16 features; its
-// NW wavefronts take runs of four k-steps (256 bytes of each of the 16 weight rows) in turn and add their
-// sums through LDS in the order of the wavefronts.
-template <bool F32, int TB, int NW>
+// Up to 16 TB rows: the weights' bytes are what counts, each read once. A workgroup owns 16 features; its
+// NW wavefronts take the 128-byte stages of k in turn, each on its own: it copies the 16 weight rows and
+// the 16 TB rows of x of a stage to LDS by direct loads (whole cache lines; the fragments' own pattern, 64
+// bytes of 16 rows, passes a CU's L1 at 16 bytes a clock: 7.7 us for 16 x 4096 x 4096 whatever the
+// bandwidth of memory), DEPTH - 1 stages ahead, and waits for its own loads by their count, without a
+// barrier. The sums meet in LDS in the order of the wavefronts. DIRECT = false reads fragments from memory.
+template <bool F32, int TB, int NW, int DEPTH, bool DIRECT>
 __global__ __launch_bounds__(NW * 64) void linear_rows_kernel(LinearParams p) {
-    constexpr int ES = F32 ? 4 : 2, CH = 16 / ES, KS = 4 * CH, RUN = 4 * KS;   // elements of a k-step, of a run
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, col = lane & 15;
+    constexpr int ES = F32 ? 4 : 2, CH = 16 / ES, KS = 4 * CH, KSTAGE = 2 * KS;   // elements of a chunk, k-step, stage
+    constexpr int U = 2 + 2 * TB, SLOT = U * 1024;   // direct loads and bytes of a stage
+    extern __shared__ __align__(16) unsigned char rows_smem[];
+    unsigned char* smem = rows_smem;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4, col = lane & 15;
     const int n0 = blockIdx.x * 16;
-    __shared__ __align__(16) float part[NW * TB * 256];
     const int wr = n0 + col < p.n ? n0 + col : p.n - 1;
     const char* wp = static_cast<const char*>(p.w) + (int64_t)wr * p.ldw * ES + g * 16;
     const char* xp[TB];
@@ -372,28 +376,82 @@ __global__ __launch_bounds__(NW * 64) void linear_rows_kernel(LinearParams p) {
     f32x4 acc[TB];
 #pragma unroll
     for (int t = 0; t < TB; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int runs = p.k / RUN;
+    const int stages = p.k / KSTAGE;
+    if constexpr (DIRECT) {
+        const char* wb = static_cast<const char*>(p.w) + (int64_t)n0 * p.ldw * ES;
+        const char* xb = static_cast<const char*>(p.x);
+        const int nleft = p.n - n0;
+        uint32_t voff[U];   // unit j: rows 8 j .. 8 j + 7 of the weights (j < 2), then of x
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int r = 8 * j + (lane >> 3);
+            const int64_t off = r < 16 ? (int64_t)(r < nleft ? r : nleft - 1) * p.ldw : (int64_t)(r - 16 < p.m ? r - 16 : p.m - 1) * p.ldx;
+            voff[j] = (uint32_t)(off * ES) + (uint32_t)(((lane & 7) ^ (lane >> 3)) * 16);
+        }
+        unsigned char* ring = smem + wave * DEPTH * SLOT;
+        auto load = [&](int i) {   // this wavefront's i-th stage
+            const int64_t at = (int64_t)(wave + i * NW) * 128;
+            const uint32_t dst = lds_addr(ring) + i % DEPTH * SLOT;
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                const char* src = uniform_ptr((j < 2 ? wb : xb) + at);
+                asm volatile(LDS_DMA_GUARD "global_load_lds_dwordx4 %0, %1" :: "v"(voff[j]), "s"(src), "{m0}"(dst + j * 1024)
+                             : "memory");
+            }
+        };
+        const int mine = wave < stages ? (stages - wave + NW - 1) / NW : 0;
+#pragma unroll
+        for (int i = 0; i < DEPTH - 1; ++i)
+            if (i < mine) load(i);
+        for (int i = 0; i < mine; ++i) {
+            // Stage i has come when at most the DEPTH - 2 behind it are under way; and this wavefront has read what
+            // it is about to overwrite.
+            if (i + DEPTH - 2 < mine) {
+                if constexpr (DEPTH == 4 && U == 4) asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)" ::: "memory");
+                else if constexpr (DEPTH == 3 && U == 6) asm volatile("s_waitcnt vmcnt(6) lgkmcnt(0)" ::: "memory");
+                else if constexpr (DEPTH == 3 && U == 10) asm volatile("s_waitcnt vmcnt(10) lgkmcnt(0)" ::: "memory");
+                else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            } else {
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            }
+            if (i + DEPTH - 1 < mine) load(i + DEPTH - 1);
+            // the lanes read what the others loaded: the slot's offset is one value of the wavefront, taken after
+            // its wait
+            const unsigned char* at = ring + __builtin_amdgcn_readfirstlane(i % DEPTH * SLOT) + col * 128;
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+                const int slot = ((ks * 4 + g) ^ (col & 7)) * 16;
+                const u32x4 a = *reinterpret_cast<const u32x4*>(at + slot);
+#pragma unroll
+                for (int t = 0; t < TB; ++t) acc[t] = mma<F32>(a, *reinterpret_cast<const u32x4*>(at + (t + 1) * 2048 + slot), acc[t]);
+            }
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
 #pragma unroll 2
-    for (int r = wave; r < runs; r += NW) {
-        u32x4 a[4], b[TB][4];
+        for (int s = wave; s < stages; s += NW) {
+            u32x4 a[2], b[TB][2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) a[j] = load16(wp + (int64_t)r * (RUN * ES) + j * 64);
+            for (int j = 0; j < 2; ++j) a[j] = load16(wp + (int64_t)s * 128 + j * 64);
 #pragma unroll
-        for (int t = 0; t < TB; ++t)
+            for (int t = 0; t < TB; ++t)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) b[t][j] = load16(xp[t] + (int64_t)r * (RUN * ES) + j * 64);
+                for (int j = 0; j < 2; ++j) b[t][j] = load16(xp[t] + (int64_t)s * 128 + j * 64);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int t = 0; t < TB; ++t) acc[t] = mma<F32>(a[j], b[t][j], acc[t]);
+                for (int t = 0; t < TB; ++t) acc[t] = mma<F32>(a[j], b[t][j], acc[t]);
+        }
     }
-    // what is left: fewer than four k-steps, the last of them possibly not whole
-    for (int j = wave; runs * RUN + j * KS < p.k; j += NW) {
-        const int k0 = runs * RUN + j * KS, left = p.k - k0 - g * CH;
+    // what is left: at most two k-steps, the last of them possibly not whole
+    for (int j = wave; stages * KSTAGE + j * KS < p.k; j += NW) {
+        const int k0 = stages * KSTAGE + j * KS, left = p.k - k0 - g * CH;
         const u32x4 a = load_chunk<F32>(wp + (int64_t)k0 * ES, left);
 #pragma unroll
         for (int t = 0; t < TB; ++t) acc[t] = mma<F32>(a, load_chunk<F32>(xp[t] + (int64_t)k0 * ES, left), acc[t]);
     }
+    __syncthreads();   // the rings are free for the sums
+    float* part = reinterpret_cast<float*>(smem);
 #pragma unroll
     for (int t = 0; t < TB; ++t) *reinterpret_cast<f32x4*>(part + ((wave * TB + t) * 64 + lane) * 4) = acc[t];
     __syncthreads();
@@ -416,10 +474,24 @@ __global__ __launch_bounds__(NW * 64) void linear_rows_kernel(LinearParams p) {
     }
 }
 
-template <bool F32, int TB, int NW>
+template <bool F32, int TB, int NW, int DEPTH, bool DIRECT>
 hipError_t rows(const LinearParams& p, hipStream_t s) {
-    linear_rows_kernel<F32, TB, NW><<<dim3((p.n + 15) / 16), dim3(NW * 64), 0, s>>>(p);
+    const int smem = NW * (DIRECT ? DEPTH * (2 + 2 * TB) : TB) * 1024;
+    const void* fn = reinterpret_cast<const void*>(&linear_rows_kernel<F32, TB, NW, DEPTH, DIRECT>);
+    const hipError_t e = smem > 65536 ? hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, smem) : hipSuccess;
+    if (e != hipSuccess) return e;
+    linear_rows_kernel<F32, TB, NW, DEPTH, DIRECT><<<dim3((p.n + 15) / 16), dim3(NW * 64), smem, s>>>(p);
     return hipGetLastError();
+}
+
+// Wavefronts and ring depth by what LDS holds: about 100 KB of a CU under way.
+template <bool F32, bool DIRECT>
+hipError_t few(const LinearParams& p, int kernel, hipStream_t s) {
+    switch (kernel) {
+        case LIN_ROWS16: return rows<F32, 1, 8, 4, DIRECT>(p, s);
+        case LIN_ROWS32: return rows<F32, 2, 8, 3, DIRECT>(p, s);
+        default: return rows<F32, 4, DIRECT ? 4 : 8, 3, DIRECT>(p, s);
+    }
 }
 
 template <bool F32, int BM, int BN, int WM, int WN, bool DIRECT>
@@ -480,23 +552,21 @@ LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, bool f32, bool in_order)
 
 int64_t linear_threads(const LinearPlan& plan, int64_t m, int64_t n) {
     const int64_t t = plan.kernel == LIN_TILE256 ? 256 : plan.kernel == LIN_TILE128 ? 128 : 64;
-    if (plan.kernel < LIN_TILE64) return (n + 15) / 16 * 1024;
+    if (plan.kernel < LIN_TILE64) return (n + 15) / 16 * 512;
     return (m + t - 1) / t * ((n + t - 1) / t) * plan.splits * (t == 256 ? 512 : 256);
 }
 
 hipError_t launch_linear(const LinearParams& p, const LinearPlan& plan, hipStream_t s) {
-    switch (plan.kernel) {
-        case LIN_ROWS16: return p.f32 ? rows<true, 1, 16>(p, s) : rows<false, 1, 16>(p, s);
-        case LIN_ROWS32: return p.f32 ? rows<true, 2, 16>(p, s) : rows<false, 2, 16>(p, s);
-        case LIN_ROWS64: return p.f32 ? rows<true, 4, 16>(p, s) : rows<false, 4, 16>(p, s);
-        default: break;
-    }
     // direct loads copy 16-byte chunks from 32-bit offsets within a tile of up to 256 rows
     const int es = p.f32 ? 4 : 2;
     auto ok = [&](const void* q, int64_t ld) {
         return reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld * es % 16 == 0 && ld * es <= (int64_t)15 << 20;
     };
     const bool direct = ok(p.x, p.ldx) && ok(p.w, p.ldw);
+    if (plan.kernel < LIN_TILE64) {
+        if (p.f32) return direct ? few<true, true>(p, plan.kernel, s) : few<true, false>(p, plan.kernel, s);
+        return direct ? few<false, true>(p, plan.kernel, s) : few<false, false>(p, plan.kernel, s);
+    }
     if (p.f32) return direct ? tiles<true, true>(p, plan.kernel, s) : tiles<true, false>(p, plan.kernel, s);
     return direct ? tiles<false, true>(p, plan.kernel, s) : tiles<false, false>(p, plan.kernel, s);
 }
