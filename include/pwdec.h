@@ -438,7 +438,7 @@ int pwd_qk_norm_rope(const pwd_rope_args* args, const float* d_gain_q, const flo
  *   (negative: no bound; window_right = 0 is causal) and the keys j < sinks up to position + window_right.
  *   A query that sees no key gives zeros.
  * head_dim up to 256, a multiple of 8 (bf16) or 4 (fp32); q_heads a multiple of k_heads; q_len, k_len up to
- * 2^30; scale > 0. bf16: the weights are rounded to bf16 for their product with v. An infinite or NaN value
+ * 2^30; scale > 0; token strides of k and v up to 2^25 bytes. bf16: the weights are rounded to bf16 for their product with v. An infinite or NaN value
  * in a row of v within the length may reach queries that do not see it. Results do not depend on the other sequences of the batch beyond their last bits: the keys are split
  * over workgroups by the sizes of the call. */
 typedef struct {

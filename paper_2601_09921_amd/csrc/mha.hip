@@ -15,6 +15,8 @@
 // a sequence's keys be zeros whatever memory holds there. Only tiles that some row of the workgroup sees
 // are visited: the sinks' and the window's. Where rows are few, runs of those tiles go to different
 // workgroups (splits), whose sums mha_join_kernel joins in their order.
+#include <type_traits>
+
 #include "common.h"
 #include "ops.h"
 
@@ -33,8 +35,7 @@ template <bool F32, int DH, int NW, int QT>
 struct Shape {
     static constexpr int ES = F32 ? 4 : 2, CH = 16 / ES;   // element bytes, elements of a 16-byte chunk
     // keys of a tile: a single wavefront stages it all, which at 256 features fits its registers by half
-    // (four wavefronts: 128 keys at small heads, where a tile's products are few beside its barrier)
-    static constexpr int KT = (F32 ? 32 : 64) * (NW == 1 && DH == 256 ? 1 : NW > 1 && DH == 32 && !F32 ? 4 : 2) / 2;
+    static constexpr int KT = (F32 ? 32 : 64) / (NW == 1 && DH == 256 ? 2 : 1);
     static constexpr int CK = DH / CH;                     // chunks of a row
     static constexpr int KSQ = CK / 4;                     // k-steps of a score: four chunks
     static constexpr int KB = KT * DH * ES, VB = KB;       // bytes of a tile of K, of V
@@ -42,8 +43,10 @@ struct Shape {
     static constexpr int SMEM = BUFS * (KB + VB);
     static constexpr int NT = NW * 64;
     static constexpr int KL = KT * CK / NT;                // chunks of K a thread stages
-    static constexpr int VN = F32 ? KT * CK : KT / 4 * CK; // pieces of V: chunks, or blocks of 4 keys x 1 chunk
-    static constexpr int VL = (VN + NT - 1) / NT;          // of which a thread stages
+    // bf16 V: a thread takes 4 keys x VF features at a time, as many features as leave every thread a piece
+    static constexpr int VF = NW == 1 || DH >= 128 ? 8 : DH / 16;
+    static constexpr int VC = F32 ? CK : DH / VF, VL = KT / 4 * VC / NT;
+    static_assert(KT * CK % NT == 0 && (F32 || KT / 4 * VC % NT == 0), "whole pieces per thread");
 };
 
 // LDS slot (16 bytes) of chunk c of row r in a tile of rows of CK chunks
@@ -61,7 +64,7 @@ PWD_DEV int vt_slot(int f, int c) {
 }
 
 template <bool F32, int DH, int NW, int QT>
-__global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? 2 : 1) void mha_kernel(MhaParams p, int row_tiles) {
+__global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? (DH == 32 ? 3 : 2) : 1) void mha_kernel(MhaParams p, int row_tiles) {
     using S = Shape<F32, DH, NW, QT>;
     constexpr int ES = S::ES, CH = S::CH, KT = S::KT, CK = S::CK, KSQ = S::KSQ, NT = S::NT;
     constexpr int ST = KT / 16;          // 16-key tiles
@@ -123,33 +126,46 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? 2 : 1) void mha_kern
         lo[t] = p.left < 0 ? 0 : clampk(pos - p.left);
     }
 
+    // A thread's place in a tile is the same in every tile: 32-bit offsets from the tile's first row (checked on
+    // the host). Tiles that end within the keys, of heads as wide as the kernel's, need no check per load.
     const char* kb = static_cast<const char*>(p.k) + (b * p.ks[0] + hk * p.ks[2]) * ES;
     const char* vb = static_cast<const char*>(p.v) + (b * p.vs[0] + hk * p.vs[2]) * ES;
-    u32x4 kh[S::KL], vh[F32 ? S::VL : 4 * S::VL];
+    constexpr int VC = S::VC, VF = S::VF, VW = F32 ? 1 : VF / 2;   // VW: 4-byte words of VF features
+    const uint32_t krow = (uint32_t)p.ks[1] * ES, vrow = (uint32_t)p.vs[1] * ES;
+    const uint32_t koff = tid / CK * krow + tid % CK * 16;
+    const uint32_t voff = F32 ? tid / CK * vrow + tid % CK * 16 : tid / VC * 4 * vrow + tid % VC * (VF * ES);
+    u32x4 kh[S::KL], vf[F32 ? S::KL : 1];
+    uint32_t vh[F32 ? 1 : S::VL][4][VW];
     auto fetch = [&](int key0) {
-        auto chunk = [&](const char* base, int64_t stride, int key, int c) {
-            return key < kl && c * CH < p.dh ? load16(base + key * stride * ES + c * 16) : u32x4{0, 0, 0, 0};
+        const char* kt = kb + (int64_t)key0 * p.ks[1] * ES;
+        const char* vt = vb + (int64_t)key0 * p.vs[1] * ES;
+        auto all = [&](auto checked) {
+            constexpr bool CHECK = decltype(checked)::value;
+            auto live = [&](int row, int feature) { return !CHECK || (key0 + row < kl && feature < p.dh); };
+#pragma unroll
+            for (int j = 0; j < S::KL; ++j) {
+                const int row = j * (NT / CK);
+                const bool in = live(tid / CK + row, tid % CK * CH);
+                const char *kr = kt + (uint64_t)row * krow, *vr = vt + (uint64_t)row * vrow;   // wavefront-uniform
+                kh[j] = in ? load16(kr + koff) : u32x4{0, 0, 0, 0};
+                if constexpr (F32) vf[j] = in ? load16(vr + voff) : u32x4{0, 0, 0, 0};
+            }
+            if constexpr (!F32) {
+#pragma unroll
+                for (int j = 0; j < S::VL; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int row = j * (NT / VC) * 4 + e;
+                        const bool in = live(tid / VC * 4 + row, tid % VC * VF);
+#pragma unroll
+                        for (int w = 0; w < VW; ++w) vh[j][e][w] = 0;
+                        const char* vr = vt + (uint64_t)row * vrow;
+                        if (in) __builtin_memcpy(vh[j][e], vr + voff, sizeof vh[j][e]);
+                    }
+            }
         };
-#pragma unroll
-        for (int j = 0; j < S::KL; ++j) {
-            const int i = tid + j * NT;
-            kh[j] = chunk(kb, p.ks[1], key0 + i / CK, i % CK);
-        }
-        if constexpr (F32) {
-#pragma unroll
-            for (int j = 0; j < S::VL; ++j) {
-                const int i = tid + j * NT;
-                vh[j] = chunk(vb, p.vs[1], key0 + i / CK, i % CK);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < S::VL; ++j) {
-                const int i = tid + j * NT;
-                if (S::VN % NT != 0 && i >= S::VN) break;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) vh[4 * j + e] = chunk(vb, p.vs[1], key0 + 4 * (i / CK) + e, i % CK);
-            }
-        }
+        if (key0 + KT <= kl && p.dh == DH) all(std::false_type{});
+        else all(std::true_type{});
     };
     auto stage = [&](unsigned char* at) {
         unsigned char* vt = at + S::KB;
@@ -157,26 +173,21 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? 2 : 1) void mha_kern
         for (int j = 0; j < S::KL; ++j) {
             const int i = tid + j * NT;
             *reinterpret_cast<u32x4*>(at + slot_of<CK>(i / CK, i % CK) * 16) = kh[j];
+            if constexpr (F32) *reinterpret_cast<u32x4*>(vt + slot_of<CK>(i / CK, i % CK) * 16) = vf[j];
         }
-        if constexpr (F32) {
-#pragma unroll
-            for (int j = 0; j < S::KL; ++j) {
-                const int i = tid + j * NT;
-                *reinterpret_cast<u32x4*>(vt + slot_of<CK>(i / CK, i % CK) * 16) = vh[j];
-            }
-        } else {
-            // block (4 keys, 8 features) -> per feature the 4 keys, at slots of key order
+        if constexpr (!F32) {
+            // piece (4 keys, VF features) -> per feature the 4 keys, at slots of key order
 #pragma unroll
             for (int j = 0; j < S::VL; ++j) {
-                const int i = tid + j * NT;
-                if (S::VN % NT != 0 && i >= S::VN) break;
-                const int kblk = i / CK, f0 = (i % CK) * 8;
+                const int i = tid + j * NT, kblk = i / VC, f0 = i % VC * VF;
                 const int c = kblk / 8 * 4 + kblk % 4, half = kblk % 8 / 4;
 #pragma unroll
-                for (int f = 0; f < 8; ++f) {
-                    auto h = [&](int e) { return (vh[4 * j + e][f >> 1] >> (16 * (f & 1))) & 0xffffu; };
-                    const u32x2 w = {h(0) | h(1) << 16, h(2) | h(3) << 16};
-                    *reinterpret_cast<u32x2*>(vt + vt_slot<KT>(f0 + f, c) * 16 + half * 8) = w;
+                for (int f = 0; f < VF; ++f) {
+                    auto pair = [&](int e) {   // feature f of keys e and e + 1
+                        const uint32_t x = vh[j][e][f >> 1], y = vh[j][e + 1][f >> 1];
+                        return f & 1 ? x >> 16 | (y & 0xffff0000u) : (x & 0xffffu) | y << 16;
+                    };
+                    *reinterpret_cast<u32x2*>(vt + vt_slot<KT>(f0 + f, c) * 16 + half * 8) = u32x2{pair(0), pair(2)};
                 }
             }
         }
@@ -209,24 +220,36 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? 2 : 1) void mha_kern
         if (it + 1 < t_end) fetch(key_of(it + 1));
         const unsigned char* vt = at + S::KB;
 
+        // Fragments are read LA steps ahead of their products, in this order (left to itself the compiler reads
+        // as many ahead as the registers hold, and a few more)
+        constexpr int LA = 3;
         f32x4 s[ST][QT];
+        {
+            constexpr int N = ST * KSQ;   // steps: (key tile, k-step)
+            u32x4 a[LA + 1];
+            auto frag = [&](int i) {
+                return *reinterpret_cast<const u32x4*>(at + slot_of<CK>(i / KSQ * 16 + col, i % KSQ * 4 + g) * 16);
+            };
 #pragma unroll
-        for (int kt = 0; kt < ST; ++kt) {
+            for (int i = 0; i < LA && i < N; ++i) a[i] = frag(i);
+            __builtin_amdgcn_sched_group_barrier(0x100, LA < N ? LA : N, 0);
 #pragma unroll
-            for (int t = 0; t < QT; ++t) s[kt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int ks = 0; ks < KSQ; ++ks) {
-                const u32x4 a = *reinterpret_cast<const u32x4*>(at + slot_of<CK>(kt * 16 + col, ks * 4 + g) * 16);
+            for (int i = 0; i < N; ++i) {
+                const int kt = i / KSQ, ks = i % KSQ;
+                if (i + LA < N) a[(i + LA) % (LA + 1)] = frag(i + LA);
 #pragma unroll
                 for (int t = 0; t < QT; ++t) {
+                    if (ks == 0) s[kt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
                     if constexpr (F32) {
-                        const f32x4 fa = __builtin_bit_cast(f32x4, a), fb = __builtin_bit_cast(f32x4, qf[ks][t]);
+                        const f32x4 fa = __builtin_bit_cast(f32x4, a[i % (LA + 1)]), fb = __builtin_bit_cast(f32x4, qf[ks][t]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) s[kt][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(fa[e], fb[e], s[kt][t], 0, 0, 0);
                     } else {
-                        s[kt][t] = mfma16x16x32(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, qf[ks][t]), s[kt][t]);
+                        s[kt][t] = mfma16x16x32(__builtin_bit_cast(bf16x8, a[i % (LA + 1)]), __builtin_bit_cast(bf16x8, qf[ks][t]), s[kt][t]);
                     }
                 }
+                if (i + LA < N) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, F32 ? 4 * QT : QT, 0);
             }
         }
         // hide keys where the tile is not in sight of every row
@@ -297,20 +320,30 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? 2 : 1) void mha_kern
                             acc[o][t] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], s[kt][t][e], acc[o][t], 0, 0, 0);
                 }
         } else {
+            constexpr int N = ST / 2 * OT;   // steps: (key pair, feature tile)
+            u32x4 a[LA + 1];
+            auto frag = [&](int i) {
+                return *reinterpret_cast<const u32x4*>(vt + vt_slot<KT>(i % OT * 16 + col, i / OT * 4 + g) * 16);
+            };
 #pragma unroll
-            for (int kp = 0; kp < ST / 2; ++kp) {
-                bf16x8 w[QT];
+            for (int i = 0; i < LA && i < N; ++i) a[i] = frag(i);
+            bf16x8 w[QT];
 #pragma unroll
-                for (int t = 0; t < QT; ++t) {
-                    w[t] = pack_b(s[2 * kp][t], s[2 * kp + 1][t]);
-                    l[t] = mfma16x16x32(ones, w[t], l[t]);
+            for (int i = 0; i < N; ++i) {
+                const int kp = i / OT, o = i % OT;
+                if (o == 0) {
+#pragma unroll
+                    for (int t = 0; t < QT; ++t) {
+                        w[t] = pack_b(s[2 * kp][t], s[2 * kp + 1][t]);
+                        l[t] = mfma16x16x32(ones, w[t], l[t]);
+                    }
                 }
+                if (i + LA < N) a[(i + LA) % (LA + 1)] = frag(i + LA);
 #pragma unroll
-                for (int o = 0; o < OT; ++o) {
-                    const u32x4 a = *reinterpret_cast<const u32x4*>(vt + vt_slot<KT>(o * 16 + col, kp * 4 + g) * 16);
-#pragma unroll
-                    for (int t = 0; t < QT; ++t) acc[o][t] = mfma16x16x32(__builtin_bit_cast(bf16x8, a), w[t], acc[o][t]);
-                }
+                for (int t = 0; t < QT; ++t) acc[o][t] = mfma16x16x32(__builtin_bit_cast(bf16x8, a[i % (LA + 1)]), w[t], acc[o][t]);
+                if (i + LA < N) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                if (o == 0) __builtin_amdgcn_sched_group_barrier(0x008, 2 * QT, 0);
+                else __builtin_amdgcn_sched_group_barrier(0x008, QT, 0);
             }
         }
     }

@@ -254,6 +254,9 @@ int pwd_attention(const pwd_attention_args* a, void* hip_stream) {
     for (const int64_t* st : {a->q_stride, a->k_stride, a->v_stride, a->out_stride})
         for (int i = 0; i < 3; ++i)
             if (st[i] < 0) return fail(PWD_EINVAL, "attention: negative stride");
+    for (const int64_t* st : {a->k_stride, a->v_stride})   // 32-bit offsets within a tile of up to 64 keys
+        if (a->k_len > 1 && st[1] > ((int64_t)1 << 25) / (int64_t)es)
+            return fail(PWD_EUNSUPPORTED, "attention: token stride %lld of the keys or values: need at most 2^25 bytes", (long long)st[1]);
     const int64_t len[3] = {a->batch, a->q_len, a->q_heads};
     for (int i = 0; i < 3; ++i)
         if (len[i] > 1 && a->out_stride[i] < a->head_dim)

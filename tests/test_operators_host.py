@@ -102,7 +102,7 @@ def attention_args(**kw):
     (dict(q_heads=3), BAD), (dict(k_heads=0), BAD), (dict(k_len=(1 << 30) + 1), NO), (dict(scale=0.0), BAD), (dict(scale=-1.0), BAD),
     (dict(scale=math.inf), BAD), (dict(scale=math.nan), BAD), (dict(d_q=None), BAD), (dict(d_v=None), BAD), (dict(d_out=None), BAD),
     (dict(d_k=PTR + 1), BAD), (dict(d_q_lengths=PTR + 2), BAD), (dict(out_stride=(1280, 128, 31)), BAD),
-    (dict(k_stride=(1280, -64, 32)), BAD), (dict(d_out=PTR), BAD), (dict(batch=1 << 30, q_len=1 << 20), NO),
+    (dict(k_stride=(1280, -64, 32)), BAD), (dict(d_out=PTR), BAD), (dict(v_stride=(1 << 40, (1 << 24) + 1, 32)), NO), (dict(batch=1 << 30, q_len=1 << 20), NO),
 ])
 def test_attention_refuses(lib, kw, rc):
     assert lib.pwd_attention(ctypes.byref(attention_args(**kw)), None) == rc
