@@ -354,8 +354,9 @@ int decoder_create_rotary(const pwd_geometry* geom, const pwd_model_dims* dims, 
  * hip_stream, and keep nothing from call to call. dtype is PWD_DTYPE_BF16 or PWD_DTYPE_F32; sums,
  * softmax statistics and norms are fp32, results are rounded once. Strides and leading dimensions
  * count elements, the last axis of every tensor is contiguous; rows may start at any element. A
- * size of zero is a no-op. Outputs must not overlap inputs except where stated. Where a workspace
- * size is given, it may be 0, and the caller allocates that many bytes of device memory (16-byte
+ * size of zero is a no-op. Outputs must not overlap inputs except where stated (PWD_EINVAL where the
+ * two start at one place or both are packed; columns of one buffer may interleave). Where a workspace
+ * size is given, it may be 0; else the caller allocates that many bytes of device memory (16-byte
  * aligned, any contents) which calls that overlap must not share. PWD_EINVAL: a null pointer, a
  * negative size, a stride smaller than the row it steps over, a workspace that is too small;
  * PWD_EUNSUPPORTED: an unknown dtype or option, or a size outside the stated range. */
@@ -438,7 +439,7 @@ int pwd_qk_norm_rope(const pwd_rope_args* args, const float* d_gain_q, const flo
  *   (negative: no bound; window_right = 0 is causal) and the keys j < sinks up to position + window_right.
  *   A query that sees no key gives zeros.
  * head_dim up to 256, a multiple of 8 (bf16) or 4 (fp32); q_heads a multiple of k_heads; q_len, k_len up to
- * 2^30; scale > 0; token strides of k and v up to 2^25 bytes. bf16: the weights are rounded to bf16 for their product with v. An infinite or NaN value
+ * 2^30; scale 1e-20..1e20; token strides of k and v up to 2^25 bytes. bf16: the weights are rounded to bf16 for their product with v. An infinite or NaN value
  * in a row of v within the length may reach queries that do not see it. Results do not depend on the other sequences of the batch beyond their last bits: the keys are split
  * over workgroups by the sizes of the call. */
 typedef struct {

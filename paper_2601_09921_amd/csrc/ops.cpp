@@ -153,7 +153,7 @@ int plan_of(const pwd_attention_args* a, MhaPlan* plan) {
                     (long long)a->batch, (long long)a->q_len, (long long)a->k_len);
     if (a->k_heads == 0 ? a->q_heads != 0 : a->q_heads % a->k_heads != 0)
         return fail(PWD_EINVAL, "attention: %d query heads over %d key heads", a->q_heads, a->k_heads);
-    if (!(a->scale > 0.0) || !std::isfinite(a->scale)) return fail(PWD_EINVAL, "attention: scale %g: need a positive number", a->scale);
+    if (!(a->scale >= 1e-20 && a->scale <= 1e20)) return fail(PWD_EINVAL, "attention: scale %g: need 1e-20..1e20", a->scale);
     *plan = MhaPlan{1, 1, 1};
     if (a->batch == 0 || a->q_len == 0 || a->q_heads == 0) return PWD_OK;
     auto cap = [](int64_t v) { return v > LEN_MAX ? LEN_MAX : v; };

@@ -85,7 +85,8 @@ def check(got, ref, bound, what=""):
 
 # (m, n, k): one row to several tiles of each kernel, sizes on and around the tiles' edges
 LINEAR_SHAPES = [(1, 1, 1), (1, 16, 64), (3, 5, 7), (16, 33, 257), (17, 40, 96), (33, 64, 128), (64, 20, 515),
-                 (65, 64, 64), (70, 100, 72), (130, 129, 200), (5, 7, 0)]
+                 (65, 64, 64), (70, 100, 72), (130, 129, 200), (5, 7, 0),
+                 (66, 40, 1100)]   # split along k
 
 # tokens, q heads, k heads, dh, pairs, layout, shared
 ROPE_SHAPES = [(1, 1, 1, 2, (1,), "half", False), (3, 2, 1, 16, (8,), "half", False), (5, 4, 2, 32, (8, 8), "half", False),
@@ -106,4 +107,5 @@ ATTENTION_SHAPES = [
     (1, 20, 150, 3, 1, 128, (30, 2), 70, None, None),
     (1, 17, 66, 2, 2, 80, (0, 0), 0, None, None),        # only its own key
     (1, 5, 64, 2, 1, 256, (-1, -1), 0, None, None),
+    (2, 2, 700, 2, 1, 16, (600, 0), 3, None, (700, 40)),  # keys split over workgroups, one of them without any
 ]

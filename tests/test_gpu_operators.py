@@ -40,7 +40,7 @@ def strided(a, dtype, pad):
 
 
 BIG = [(300, 200, 1000), (1, 1000, 4096), (48, 512, 2050), (129, 1024, 4096), (513, 257, 130), (1500, 2048, 192), (4100, 1031, 65),
-       (2560, 2560, 128)]
+       (2560, 2560, 128), (4096, 4100, 70)]
 
 
 @pytest.mark.parametrize("dtype,out,act,pad", [("bf16", "bf16", "relu", 0), ("bf16", "fp32", "gelu", 3), ("fp32", "fp32", "silu", 0),
@@ -98,6 +98,84 @@ def test_rope_inverse_undoes_the_rotation():
     assert np.abs(host(q) - x).max() > 0.5
     pwdec.rope(q, None, dev(pos), (10, 11, 11), inverse=True)
     C.check(host(q), x.astype(np.float64), 4 * C.rope_bound(x.astype(np.float64), x, "fp32", (10, 11, 11), "half"))
+
+
+def test_rope_of_keys_alone():
+    """Keys without queries, one axis given as [tokens], against the same call with both."""
+    rng = np.random.default_rng(6)
+    x, pos = C.values(rng, (9, 2, 32), "bf16"), dev(rng.integers(0, 99, 9).astype(np.int32))
+    a, b, c = dev(x, "bf16"), dev(x, "bf16"), torch.empty(9, 2, 32, dtype=torch.bfloat16, device="cuda")
+    pwdec.rope(a, b, pos, (16,))
+    pwdec.rope(None, c.copy_(dev(x, "bf16")), pos[:, None], (16,))
+    assert torch.equal(a, b) and torch.equal(a, c)
+    g = torch.ones(32, device="cuda")
+    pwdec.qk_norm_rope(None, c.copy_(dev(x, "bf16")), None, g, pos, (16,))
+    pwdec.qk_norm_rope(a.copy_(dev(x, "bf16")), None, None, None, pos, (16,))
+    assert torch.equal(a, c)
+
+
+def test_offsets_past_32_bits():
+    """Rows, tokens and sequences more than 2^31 elements into their buffers."""
+    rng = np.random.default_rng(8)
+    big = torch.empty((1 << 31) + (1 << 22), dtype=torch.bfloat16, device="cuda")   # 4 GB, each row at a stride
+    ld = 1 << 21
+    for m in (40, 1025):   # the kernel for few rows, and the tiles
+        x = big.as_strided((m, 64), (ld if m > 64 else (1 << 31) // 39, 1))
+        a, w = C.values(rng, (m, 64), "bf16"), C.values(rng, (30, 64), "bf16")
+        x.copy_(dev(a, "bf16"))
+        y = torch.empty(m, 30, device="cuda")
+        pwdec.linear(x, dev(w, "bf16"), y)
+        ref, mag = O.linear(a, w)
+        C.check(host(y), ref, C.linear_bound(ref, mag, 64, "none", "fp32", None))
+        out = big.as_strided((m, 64), (ld if m > 64 else (1 << 31) // 39, 1))
+        pwdec.linear(dev(a, "bf16"), dev(np.eye(64, dtype=np.float32), "bf16"), out)
+        assert torch.equal(out, dev(a, "bf16"))
+    t = C.values(rng, (3, 2, 32), "bf16")
+    q = big.as_strided((3, 2, 32), (1 << 30, 32, 1))
+    q.copy_(dev(t, "bf16"))
+    pos = np.array([[3], [5], [1 << 20]], np.int32)
+    pwdec.rope(q, None, dev(pos), (16,))
+    ref = O.rope(t, pos, (16,))
+    C.check(host(q), ref, C.rope_bound(ref, t, "bf16", (16,), "half"))
+    kv, qq = C.values(rng, (3, 100, 1, 32), "bf16"), C.values(rng, (3, 1, 1, 32), "bf16")
+    cache = big.as_strided((3, 100, 1, 32), (1 << 30, 4096, 32, 1))
+    cache.copy_(dev(kv, "bf16"))
+    out = torch.empty(3, 1, 1, 32, dtype=torch.bfloat16, device="cuda")
+    pwdec.attention(dev(qq, "bf16"), cache, cache, out)
+    ref, mag, top = O.attention(qq, kv, kv)
+    C.check(host(out), ref, C.attention_bound(ref, mag, top, "bf16", 32, 100))
+    keys = big.as_strided((1, 300, 1, 32), (0, (1 << 31) // 299 // 8 * 8, 32, 1))   # one sequence, far apart tokens
+    kv = C.values(rng, (1, 300, 1, 32), "bf16")
+    keys.copy_(dev(kv, "bf16"))
+    pwdec.attention(dev(qq[:1], "bf16"), keys, keys, out[:1])
+    ref, mag, top = O.attention(qq[:1], kv, kv)
+    C.check(host(out[:1]), ref, C.attention_bound(ref, mag, top, "bf16", 32, 300))
+
+
+def test_workspaces_and_streams_that_are_given():
+    """A workspace of the caller's gives the same result; one too small, of another type, or a call whose tensors
+    do not fit is refused before anything runs."""
+    q, c = torch.randn(1, 1, 4, 64, device="cuda"), torch.randn(1, 4000, 2, 64, device="cuda")
+    a, b = torch.empty_like(q), torch.empty_like(q)
+    need = pwdec.attention_workspace(q, c, c, a)
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    pwdec.attention(q, c, c, a)
+    pwdec.attention(q, c, c, b, workspace=ws)
+    assert need > 0 and torch.equal(a, b)
+    x, w = torch.randn(100, 4096, device="cuda"), torch.randn(300, 4096, device="cuda")
+    y, z = torch.empty(100, 300, device="cuda"), torch.empty(100, 300, device="cuda")
+    need = pwdec.linear_workspace(x, w, y)
+    pwdec.linear(x, w, y)
+    pwdec.linear(x, w, z, workspace=torch.full((need,), 255, dtype=torch.uint8, device="cuda"))
+    assert need > 0 and torch.equal(y, z)
+    with pytest.raises(ValueError):
+        pwdec.linear(x, w, y, workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(ValueError):
+        pwdec.attention(q, c, c, b, workspace=torch.empty(1 << 20, device="cuda"))
+    with pytest.raises(pwdec.PwdError):
+        pwdec.linear(x, w, x[:, :300])
+    with pytest.raises(pwdec.PwdError):
+        pwdec.attention(q, c, c, a, scale=0.0)
 
 
 ATT_BIG = [(2, 200, 200, 4, 2, 128, (-1, 0), 0, (200, 150), (200, 150)), (1, 1, 3000, 8, 1, 128, (-1, 0), 0, None, (2900,)),

@@ -99,7 +99,7 @@ def attention_args(**kw):
 @pytest.mark.parametrize("kw,rc", [
     (dict(batch=-1), BAD), (dict(q_len=-1), BAD), (dict(k_len=-1), BAD), (dict(sinks=-1), BAD), (dict(dtype=2), NO),
     (dict(head_dim=0), NO), (dict(head_dim=12), NO), (dict(head_dim=264), NO), (dict(dtype=0, head_dim=6), NO),
-    (dict(q_heads=3), BAD), (dict(k_heads=0), BAD), (dict(k_len=(1 << 30) + 1), NO), (dict(scale=0.0), BAD), (dict(scale=-1.0), BAD),
+    (dict(q_heads=3), BAD), (dict(k_heads=0), BAD), (dict(k_len=(1 << 30) + 1), NO), (dict(scale=0.0), BAD), (dict(scale=-1.0), BAD), (dict(scale=1e-21), BAD), (dict(scale=1e21), BAD),
     (dict(scale=math.inf), BAD), (dict(scale=math.nan), BAD), (dict(d_q=None), BAD), (dict(d_v=None), BAD), (dict(d_out=None), BAD),
     (dict(d_k=PTR + 1), BAD), (dict(d_q_lengths=PTR + 2), BAD), (dict(out_stride=(1280, 128, 31)), BAD),
     (dict(k_stride=(1280, -64, 32)), BAD), (dict(d_out=PTR), BAD), (dict(v_stride=(1 << 40, (1 << 24) + 1, 32)), NO), (dict(batch=1 << 30, q_len=1 << 20), NO),
