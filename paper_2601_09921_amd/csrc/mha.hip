@@ -8,7 +8,7 @@
 // registers and the four lane groups, so a row's statistics cost one in-lane reduction and two lane
 // swaps, and the weights are the B operand of out^T = V^T P^T as they stand:
 //   bf16: two 16-key tiles make the 32-deep k-step with slots kslot(g, i) (common.h); V^T is staged in
-//         that key order. The weights are rounded to bf16 for that product (their sum is not).
+//         that key order, its features dealt to the tiles in turn, so that a lane's outputs lie together. The weights are rounded to bf16 for that product (their sum is not).
 //   fp32: register e of a 16-key tile is the k-step of v_mfma_f32_16x16x4_f32 with keys 4 g + e, V as is.
 // Keys and values go global -> registers -> LDS, a tile ahead of the one that is multiplied, which lets
 // V be transposed on the way (four keys x 8 features a thread), rows start at any alignment and rows past
@@ -55,13 +55,15 @@ PWD_DEV int slot_of(int r, int c) {
     if constexpr (CK >= 8) return r * CK + (c ^ (r & 7));
     else return r * CK + (c ^ ((r >> 1) & (CK - 1)));
 }
-// of V^T (bf16): row = feature, chunks of 8 keys; 8 features of one load differ in the low bits, the
-// loads' features in the next
+// of V^T (bf16): row f of chunks of 8 keys
 template <int KT>
 PWD_DEV int vt_slot(int f, int c) {
     constexpr int N = KT / 8;
-    return f * N + (c ^ ((N >= 8 ? f ^ (f >> 3) : (f >> 1) ^ (f >> 3)) & (N < 8 ? N - 1 : 7)));
+    return f * N + (c ^ ((N >= 8 ? f : f >> 1) & (N < 8 ? N - 1 : 7)));
 }
+// Block of 4 keys that the n-th piece of V along the keys is: neighbouring pieces take turns at the two halves
+// of a chunk, so that a wavefront's writes spread over all banks (a permutation of n's bits).
+PWD_DEV int key_block(int n) { return (n & 8) | (n & 1) << 2 | (n >> 1 & 3); }
 
 template <bool F32, int DH, int NW, int QT>
 __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? (DH == 32 ? 3 : 2) : 1) void mha_kernel(MhaParams p, int row_tiles) {
@@ -133,7 +135,7 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? (DH == 32 ? 3 : 2) :
     constexpr int VC = S::VC, VF = S::VF, VW = F32 ? 1 : VF / 2;   // VW: 4-byte words of VF features
     const uint32_t krow = (uint32_t)p.ks[1] * ES, vrow = (uint32_t)p.vs[1] * ES;
     const uint32_t koff = tid / CK * krow + tid % CK * 16;
-    const uint32_t voff = F32 ? tid / CK * vrow + tid % CK * 16 : tid / VC * 4 * vrow + tid % VC * (VF * ES);
+    const uint32_t voff = F32 ? tid / CK * vrow + tid % CK * 16 : key_block(tid / VC) * 4 * vrow + tid % VC * (VF * ES);
     u32x4 kh[S::KL], vf[F32 ? S::KL : 1];
     uint32_t vh[F32 ? 1 : S::VL][4][VW];
     auto fetch = [&](int key0) {
@@ -155,8 +157,8 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? (DH == 32 ? 3 : 2) :
                 for (int j = 0; j < S::VL; ++j)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int row = j * (NT / VC) * 4 + e;
-                        const bool in = live(tid / VC * 4 + row, tid % VC * VF);
+                        const int row = key_block(j * (NT / VC)) * 4 + e;
+                        const bool in = live(key_block(tid / VC) * 4 + row, tid % VC * VF);
 #pragma unroll
                         for (int w = 0; w < VW; ++w) vh[j][e][w] = 0;
                         const char* vr = vt + (uint64_t)row * vrow;
@@ -179,7 +181,7 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? (DH == 32 ? 3 : 2) :
             // piece (4 keys, VF features) -> per feature the 4 keys, at slots of key order
 #pragma unroll
             for (int j = 0; j < S::VL; ++j) {
-                const int i = tid + j * NT, kblk = i / VC, f0 = i % VC * VF;
+                const int i = tid + j * NT, kblk = key_block(i / VC), f0 = i % VC * VF;
                 const int c = kblk / 8 * 4 + kblk % 4, half = kblk % 8 / 4;
 #pragma unroll
                 for (int f = 0; f < VF; ++f) {
@@ -187,7 +189,8 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? (DH == 32 ? 3 : 2) :
                         const uint32_t x = vh[j][e][f >> 1], y = vh[j][e + 1][f >> 1];
                         return f & 1 ? x >> 16 | (y & 0xffff0000u) : (x & 0xffffu) | y << 16;
                     };
-                    *reinterpret_cast<u32x2*>(vt + vt_slot<KT>(f0 + f, c) * 16 + half * 8) = u32x2{pair(0), pair(2)};
+                    const int row = (f0 + f) % OT * 16 + (f0 + f) / OT;   // feature m OT + o is row m of tile o
+                    *reinterpret_cast<u32x2*>(vt + vt_slot<KT>(row, c) * 16 + half * 8) = u32x2{pair(0), pair(2)};
                 }
             }
         }
@@ -362,8 +365,10 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? (DH == 32 ? 3 : 2) :
 #pragma unroll
             for (int f = 0; f < OT; ++f)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (f * 16 + 4 * g + i < p.dh) o[f * 16 + 4 * g + i] = acc[f][t][i];
+                for (int i = 0; i < 4; ++i) {
+                    const int at = F32 ? f * 16 + 4 * g + i : (4 * g + i) * OT + f;
+                    if (at < p.dh) o[at] = acc[f][t][i];
+                }
             if (g == 0) {
                 float* ml = p.partial + (int64_t)p.splits * all_rows * p.dh + ((int64_t)split * all_rows + row) * 2;
                 ml[0] = m[t] * p.scale2;
@@ -372,21 +377,30 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? (DH == 32 ? 3 : 2) :
         } else {
             const float inv = sum > 0.f || sum != sum ? 1.f / sum : 0.f;   // a row that sees nothing: zeros
             char* o = static_cast<char*>(p.out) + (b * p.os[0] + tok * p.os[1] + head * p.os[2]) * ES;
+            if constexpr (F32) {
 #pragma unroll
-            for (int f = 0; f < OT; ++f) {
-                const int c = f * 16 + 4 * g;
-                if (c >= p.dh) continue;   // heads are whole multiples of 4 features
-                if constexpr (F32) {
+                for (int f = 0; f < OT; ++f) {
+                    const int c = f * 16 + 4 * g;
+                    if (c >= p.dh) continue;   // heads are whole multiples of 4 features
                     f32x4 v;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) v[i] = acc[f][t][i] * inv;
                     __builtin_memcpy(o + c * 4, &v, 16);
-                } else {
-                    bf16x4 v;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = (__bf16)(acc[f][t][i] * inv);
-                    __builtin_memcpy(o + c * 2, &v, 8);
                 }
+            } else {
+                constexpr int W = OT < 8 ? OT : 8;   // heads are whole multiples of 8 features
+                typedef __bf16 vec __attribute__((ext_vector_type(W)));
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int f = 0; f < OT; f += W) {
+                        const int c = (4 * g + i) * OT + f;
+                        if (c >= p.dh) continue;
+                        vec v;
+#pragma unroll
+                        for (int e = 0; e < W; ++e) v[e] = (__bf16)(acc[f + e][t][i] * inv);
+                        __builtin_memcpy(o + c * 2, &v, sizeof v);
+                    }
             }
         }
     }
