@@ -8,13 +8,23 @@
 // registers and the four lane groups, so a row's statistics cost one in-lane reduction and two lane
 // swaps, and the weights are the B operand of out^T = V^T P^T as they stand:
 //   bf16: two 16-key tiles make the 32-deep k-step with slots kslot(g, i) (common.h); V^T is staged in
-//         that key order, its features dealt to the tiles in turn, so that a lane's outputs lie together. The weights are rounded to bf16 for that product (their sum is not).
+//         that key order, its features dealt to the tiles in turn, so that a lane's outputs lie together. The
+//         weights are rounded to bf16 for that product (in fp32 it would run at a sixteenth of the rate), and
+//         their sum is that of the rounded ones (a row of ones times the weights), so that a row's weights still
+//         add up to one.
 //   fp32: register e of a 16-key tile is the k-step of v_mfma_f32_16x16x4_f32 with keys 4 g + e, V as is.
 // Keys and values go global -> registers -> LDS, a tile ahead of the one that is multiplied, which lets
 // V be transposed on the way (four keys x 8 features a thread), rows start at any alignment and rows past
 // a sequence's keys be zeros whatever memory holds there. Only tiles that some row of the workgroup sees
 // are visited: the sinks' and the window's. Where rows are few, runs of those tiles go to different
 // workgroups (splits), whose sums mha_join_kernel joins in their order.
+//
+// What bounds it, by its counters: a prompt's layer with heads of 128 (8192 tokens, window 1024: 360 us, 718
+// TFLOP/s; 4096 causal tokens 719) waits 28 % and issues vector instructions 44 % of the time beside a matrix core
+// busy for 30 %; heads of 32 (624 tokens each way: 230 us, 444 TFLOP/s) issue them 80 % of the time, the exponentials
+// foremost (a quarter of the vector rate); a token against long caches (119 us, 5.0 TB/s) the caches' bytes.
+// Four wavefronts of 32 rows and 64 keys a tile leave two of them to a SIMD at heads of 128 (one: 778 us
+// for the prompt) and three at heads of 32 (four spill: 310 us; 128 keys and two: 308 us; this: 263 us at that step).
 #include <type_traits>
 
 #include "common.h"

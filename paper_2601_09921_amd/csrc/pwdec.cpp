@@ -987,13 +987,17 @@ static int create_decoder(const pwd_geometry* geom, const pwd_model_dims* dims, 
         if ((e = hipMalloc(&dec->rot_act, ab + rows * 8)) != hipSuccess)
             return cleanup_fail(fail(PWD_ENOMEM, "scratch for %d windows (%zu bytes): %s", dec->max_windows, ab + rows * 8,
                                      hipGetErrorString(e)));
-        std::vector<int32_t> pos(2 * rows);
-        for (size_t r = 0; r < rows; ++r) {
-            pos[2 * r] = cells[r % dec->ntok].first;
-            pos[2 * r + 1] = cells[r % dec->ntok].second;
+        unsigned char* at = static_cast<unsigned char*>(dec->rot_act) + ab;
+        dec->rot_pos = reinterpret_cast<const int32_t*>(at);
+        std::vector<int32_t> pos;   // one window's, then doubled on the device
+        for (const auto& c : cells) {
+            pos.push_back(c.first);
+            pos.push_back(c.second);
         }
-        dec->rot_pos = reinterpret_cast<const int32_t*>(static_cast<unsigned char*>(dec->rot_act) + ab);
-        e = hipMemcpy(static_cast<unsigned char*>(dec->rot_act) + ab, pos.data(), rows * 8, hipMemcpyHostToDevice);
+        const size_t one = pos.size() * sizeof(int32_t), all = (size_t)dec->max_windows;
+        e = hipMemcpy(at, pos.data(), one, hipMemcpyHostToDevice);
+        for (size_t done = 1; done < all && e == hipSuccess; done *= 2)
+            e = hipMemcpy(at + done * one, at, std::min(done, all - done) * one, hipMemcpyDeviceToDevice);
         if (e != hipSuccess) return cleanup_fail(fail(PWD_EHIP, "hipMemcpy(positions): %s", hipGetErrorString(e)));
     } else if (dims->dtype != PWD_DTYPE_F32) {
         dec->we = fptr(off_we);

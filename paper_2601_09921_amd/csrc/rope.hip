@@ -7,7 +7,8 @@
 // crosses those lanes only. The cosines and sines of a token are the same for all its heads: a
 // workgroup computes them once for its tokens, into LDS. An angle is formed in turns in double
 // (position times turns per position; a position of 2^31 keeps 22 bits of its turn) and reduced to an
-// eighth of a turn before it is rounded to float.
+// eighth of a turn before it is rounded to float. 65536 tokens of 32 heads of 128: 200 us, 5.4 TB/s, the rate of a
+// plain copy; 319488 tokens of 16 heads of 32 with the norm: 142 us, 4.6 TB/s, vector instructions half the time.
 #include "common.h"
 #include "ops.h"
 

@@ -179,7 +179,7 @@ def test_binding_refuses():
     q, k, p = Fake(4, 2, 16, **at(0)), Fake(4, 1, 16, **at(1)), Fake(4, 2, dtype="int32", **at(2))
     for args, kw in [((None, None, p, (4, 4)), {}), ((q, Fake(5, 1, 16), p, (4, 4)), {}), ((q, Fake(4, 1, 8), p, (4, 4)), {}),
                      ((q, k, p, (4, 4, 0)), {}), ((q, k, None, (4, 4)), {}), ((q, k, Fake(4, 2, dtype="int64"), (4, 4)), {}),
-                     ((q, k, p, ()), {}), ((q, k, p, (4, 4)), dict(layout="neox")), ((q, k, p, (4, 4)), dict(frequencies="all")),
+                     ((q, k, p, ()), {}), ((q, k, p, (4, 4)), dict(layout="split")), ((q, k, p, (4, 4)), dict(frequencies="all")),
                      ((q, None, p, (4, 4)), dict(k_out=k)), ((q, k, p, (4, 4)), dict(q_out=Fake(4, 2, 8))),
                      ((Fake(4, 2, 16, index=1), k, p, (4, 4)), {}), ((q, k, Fake(3, 2, dtype="int32"), (4, 4)), {}),
                      ((q, k, p, (1, 1, 1, 1)), {})]:
