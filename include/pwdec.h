@@ -328,7 +328,9 @@ int decoder_destroy(pwd_decoder* dec);
  * max(n_tokens, distance^2) * max(d_model, 64) below 2^32; PWD_DTYPE_BF16 or PWD_DTYPE_F32; d_model a multiple of 16 in 16..1024 and a head size
  * that is a multiple of 8 (bf16) or 4 (fp32) up to 256 (d_model 192 with 8 heads of 24, the
  * hyperparameter table's, among them); mlp_ratio, n_layers, token_set, embedder as there; no dilated
- * convolutions. The entry points of the handle are the same; it has the one schedule
+ * convolutions. The entry points of the handle are the same (decode_windows_noalloc takes the batches whose
+ * activations fit its scratch, about 14 d_model + 2 F bytes a token in bf16 and 20 d_model + 4 F in fp32, and
+ * returns PWD_EBATCH for larger ones); it has the one schedule
  * PWD_SCHEDULE_LAYERS, and the stages of decoder_profile are: EMBED_QKV the embedding and fold, POST_QKV
  * the Q/K/V projection with norm and rotation, ATTENTION, OUT_PROJ, POST the feed-forward, READOUT.
  * Blob: header word 14 = qk_norm | pairs[0] << 8 | pairs[1] << 16, word 15 = theta (float32 bits);

@@ -141,7 +141,7 @@ PWD_DEV void load_bias(const LinearParams& p, int col, float* b) {
 // 4 FT (r / 4) + 4 f + r % 4, an order the loads apply when they fill the LDS rows.
 //
 // Measured at 16384 x 8192 x 4096 bf16 with 256 x 256 tiles: 836 us, 1315 TFLOP/s (8192^3: 1354), where this card's
-// library product makes 1350 to 1540. Counters: matrix core busy 62 % of the time at 1.98 GHz, LDS reads at 59 of
+// library product makes 1350 to 1540. Counters: matrix core busy 62 % of the time at 1.98 GHz, LDS reads at 60 of
 // 256 bytes a clock, no bank conflicts, wavefronts waiting 33 %: what bounds it is the wait for a stage's loads at
 // its barrier (with every load hitting L2: 1460). Not kept: 128 x 128 tiles, two workgroups a CU, 1128; 256 x 128 with
 // 64-byte stages, two a CU, 1041; four wavefronts of 128 x 128, 920 (the accumulators fill every AGPR and are copied);
@@ -434,7 +434,6 @@ __global__ __launch_bounds__(NW * 64) void linear_rows_kernel(LinearParams p) {
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     } else {
-#pragma unroll 2
         for (int s = wave; s < stages; s += NW) {
             u32x4 a[2], b[TB][2];
 #pragma unroll
@@ -517,11 +516,9 @@ hipError_t tile(const LinearParams& p, hipStream_t s) {
 
 template <bool F32, bool DIRECT>
 hipError_t tiles(const LinearParams& p, int kernel, hipStream_t s) {
-    switch (kernel) {
-        case LIN_TILE256: return tile<F32, 256, 256, 2, 4, DIRECT>(p, s);
-        case LIN_TILE128: return tile<F32, 128, 128, 2, 2, DIRECT>(p, s);
-        default: return tile<F32, 64, 64, 2, 2, DIRECT>(p, s);
-    }
+    if constexpr (!F32)
+        if (kernel == LIN_TILE256) return tile<F32, 256, 256, 2, 4, DIRECT>(p, s);
+    return kernel == LIN_TILE128 ? tile<F32, 128, 128, 2, 2, DIRECT>(p, s) : tile<F32, 64, 64, 2, 2, DIRECT>(p, s);
 }
 
 }  // namespace
@@ -529,23 +526,25 @@ hipError_t tiles(const LinearParams& p, int kernel, hipStream_t s) {
 // The kernel and the splits along k. Up to 64 rows the weights' bytes count, and the kernel for few rows
 // takes them. Beyond, the cheapest of the tiles and splits by this estimate of the product's time in
 // microseconds: a CU runs `most` workgroups of a tile side by side; one of them takes `alone` per stage
-// of k by its loads' latency, and all of them at least `each` apiece by LDS and the matrix core (256: 1.6
-// measured at 16384 x 8192 x 4096; 64: 0.45 alone at 128 x 4096 x 4096). Splits add a launch and the partial
+// of k by its loads' latency, and all of them at least `each` apiece by LDS and the matrix core (at
+// 16384 x 8192 x 4096: 256-tiles 1.6 and 128-tiles 0.48 in bf16; in fp32 128-tiles 1.84, and 256-tiles 7.6, more than
+// four of those, so they are bf16's alone; 64-tiles 0.45 alone at 128 x 4096 x 4096). Splits add a launch and the partial
 // sums' way to memory and back.
 LinearPlan linear_plan(int64_t m, int64_t n, int64_t k, bool f32, bool in_order) {
     if (!in_order && m <= 64) return {m <= 16 ? LIN_ROWS16 : m <= 32 ? LIN_ROWS32 : LIN_ROWS64, 1};
-    struct Tile { int kernel, edge, most; double each; };
-    static constexpr Tile tiles[] = {{LIN_TILE256, 256, 1, 1.6}, {LIN_TILE128, 128, 2, 0.5}, {LIN_TILE64, 64, 4, 0.22}};
-    const double stages = std::ceil((double)k / (f32 ? 32 : 64)), alone = 0.45, slow = f32 ? 3.5 : 1.0;
+    struct Tile { int kernel, edge, most; double each, each_f32; };
+    static constexpr Tile tiles[] = {{LIN_TILE256, 256, 1, 1.6, 0.0}, {LIN_TILE128, 128, 2, 0.5, 1.84}, {LIN_TILE64, 64, 4, 0.22, 0.5}};
+    const double stages = std::ceil((double)k / (f32 ? 32 : 64)), alone = 0.45;
     LinearPlan best = {LIN_TILE64, 1};
     double least = 1e300;
     for (const Tile& t : tiles) {
+        if (f32 && t.kernel == LIN_TILE256) continue;
         const double count = std::ceil((double)m / t.edge) * std::ceil((double)n / t.edge);
         for (int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
             if (splits > 1 && (in_order || stages < 4 * splits || count * splits > 1024)) break;
             const double groups = count * splits, rounds = std::ceil(groups / (256.0 * t.most));
             const double beside = std::min((double)t.most, std::ceil(groups / 256.0));
-            double time = rounds * std::ceil(stages / splits) * std::max(alone, beside * t.each * slow);
+            double time = rounds * std::ceil(stages / splits) * std::max(alone, beside * (f32 ? t.each_f32 : t.each));
             if (splits > 1) time += 4.0 + 8.0 * (double)m * (double)n * splits / 4e6;
             if (time < least) {
                 least = time;

@@ -20,8 +20,8 @@
 // workgroups (splits), whose sums mha_join_kernel joins in their order.
 //
 // What bounds it, by its counters: a prompt's layer with heads of 128 (8192 tokens, window 1024: 360 us, 718
-// TFLOP/s; 4096 causal tokens 719) waits 28 % and issues vector instructions 44 % of the time beside a matrix core
-// busy for 30 %; heads of 32 (624 tokens each way: 230 us, 444 TFLOP/s) issue them 80 % of the time, the exponentials
+// TFLOP/s; 4096 causal tokens 719) waits 29 % and issues vector instructions 50 % of the time beside a matrix core
+// busy for 34 %; heads of 32 (624 tokens each way: 230 us, 444 TFLOP/s) issue them 80 % of the time, the exponentials
 // foremost (a quarter of the vector rate); a token against long caches (119 us, 5.0 TB/s) the caches' bytes.
 // Four wavefronts of 32 rows and 64 keys a tile leave two of them to a SIMD at heads of 128 (one: 778 us
 // for the prompt) and three at heads of 32 (four spill: 310 us; 128 keys and two: 308 us; this: 263 us at that step).

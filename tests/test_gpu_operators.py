@@ -19,6 +19,10 @@ DT = {"bf16": torch.bfloat16, "fp32": torch.float32}
 def need_gpu():
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
+    before = torch.get_default_dtype()   # other modules may have left theirs
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
 
 
 def dev(a, dtype=None):

@@ -18,6 +18,10 @@ pytestmark = pytest.mark.gpu
 def need_gpu():
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
+    before = torch.get_default_dtype()   # other modules may have left theirs
+    torch.set_default_dtype(torch.float32)
+    yield
+    torch.set_default_dtype(before)
 
 
 def run(dec, fn, meas, types, k=1):
