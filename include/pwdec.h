@@ -359,7 +359,8 @@ int decoder_create_rotary(const pwd_geometry* geom, const pwd_model_dims* dims, 
  * size of zero is a no-op. Outputs must not overlap inputs except where stated (PWD_EINVAL where the
  * two start at one place or both are packed; columns of one buffer may interleave). Where a workspace
  * size is given, it may be 0; else the caller allocates that many bytes of device memory (16-byte
- * aligned, any contents) which calls that overlap must not share. PWD_EINVAL: a null pointer, a
+ * aligned, any contents), which calls that overlap, captured graphs replayed side by side among
+ * them, must not share. PWD_EINVAL: a null pointer, a
  * negative size, a stride smaller than the row it steps over, a workspace that is too small;
  * PWD_EUNSUPPORTED: an unknown dtype or option, or a size outside the stated range. */
 
