@@ -442,9 +442,11 @@ int pwd_qk_norm_rope(const pwd_rope_args* args, const float* d_gain_q, const flo
  *   (negative: no bound; window_right = 0 is causal) and the keys j < sinks up to position + window_right.
  *   A query that sees no key gives zeros.
  * head_dim up to 256, a multiple of 8 (bf16) or 4 (fp32); q_heads a multiple of k_heads; q_len, k_len up to
- * 2^30; scale 1e-20..1e20; token strides of k and v up to 2^25 bytes. bf16: the weights are rounded to bf16 for their product with v. An infinite or NaN value
- * in a row of v within the length may reach queries that do not see it. Results do not depend on the other sequences of the batch beyond their last bits: the keys are split
- * over workgroups by the sizes of the call. */
+ * 2^30; scale 1e-20..1e20; token strides of k and v up to 2^25 bytes. bf16: the weights are rounded to bf16
+ * for their product with v, and add up as rounded. Keys that no query of their sequence sees may hold anything;
+ * an infinite or NaN value in a row of v that some query sees may reach queries near it that do not. Results
+ * depend on the sizes of the call (how the keys are split over workgroups) in their last bits, not on
+ * the other sequences' contents. */
 typedef struct {
     int64_t batch, q_len, k_len;
     int32_t q_heads, k_heads, head_dim, dtype;

@@ -14,8 +14,8 @@
 //         add up to one.
 //   fp32: register e of a 16-key tile is the k-step of v_mfma_f32_16x16x4_f32 with keys 4 g + e, V as is.
 // Keys and values go global -> registers -> LDS, a tile ahead of the one that is multiplied, which lets
-// V be transposed on the way (four keys x 8 features a thread), rows start at any alignment and rows past
-// a sequence's keys be zeros whatever memory holds there. Only tiles that some row of the workgroup sees
+// V be transposed on the way (four keys x up to 8 features a thread), rows start at any alignment and keys
+// that no row of the workgroup sees be zeros whatever memory holds there. Only tiles that some row of the workgroup sees
 // are visited: the sinks' and the window's. Where rows are few, runs of those tiles go to different
 // workgroups (splits), whose sums mha_join_kernel joins in their order.
 //
@@ -139,7 +139,8 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? (DH == 32 ? 3 : 2) :
     }
 
     // A thread's place in a tile is the same in every tile: 32-bit offsets from the tile's first row (checked on
-    // the host). Tiles that end within the keys, of heads as wide as the kernel's, need no check per load.
+    // the host). Keys that no row of the workgroup sees are zeros, so that what memory holds
+    // there reaches no sum; tiles without any, of heads as wide as the kernel's, need no check per load.
     const char* kb = static_cast<const char*>(p.k) + (b * p.ks[0] + hk * p.ks[2]) * ES;
     const char* vb = static_cast<const char*>(p.v) + (b * p.vs[0] + hk * p.vs[2]) * ES;
     constexpr int VC = S::VC, VF = S::VF, VW = F32 ? 1 : VF / 2;   // VW: 4-byte words of VF features
@@ -153,7 +154,10 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? (DH == 32 ? 3 : 2) :
         const char* vt = vb + (int64_t)key0 * p.vs[1] * ES;
         auto all = [&](auto checked) {
             constexpr bool CHECK = decltype(checked)::value;
-            auto live = [&](int row, int feature) { return !CHECK || (key0 + row < kl && feature < p.dh); };
+            auto live = [&](int row, int feature) {
+                const int key = key0 + row;
+                return !CHECK || (key < hi_any && (key >= lo_any || key < p.sinks) && feature < p.dh);
+            };
 #pragma unroll
             for (int j = 0; j < S::KL; ++j) {
                 const int row = j * (NT / CK);
@@ -176,7 +180,7 @@ __global__ __launch_bounds__(NW * 64, NW > 1 && DH <= 128 ? (DH == 32 ? 3 : 2) :
                     }
             }
         };
-        if (key0 + KT <= kl && p.dh == DH) all(std::false_type{});
+        if (key0 + KT <= hi_any && (key0 >= lo_any || key0 + KT <= p.sinks) && p.dh == DH) all(std::false_type{});
         else all(std::true_type{});
     };
     auto stage = [&](unsigned char* at) {

@@ -73,6 +73,14 @@ def attention_bound(ref, mag, top, dtype, dh, keys):
     return e + H[dtype] * (np.abs(ref) + e)
 
 
+def seen_keys(n_q, n_k, k_len, window, sinks):
+    """bool [k_len]: the keys that any of the n_q queries of a sequence of n_k keys sees."""
+    seen = np.zeros(k_len, bool)
+    for i in range(n_q):
+        seen[:n_k] |= O.visible(i, n_q, n_k, *window, sinks)
+    return seen
+
+
 def check(got, ref, bound, what=""):
     got = np.asarray(got, np.float64)
     assert got.shape == ref.shape
@@ -107,5 +115,6 @@ ATTENTION_SHAPES = [
     (1, 20, 150, 3, 1, 128, (30, 2), 70, None, None),
     (1, 17, 66, 2, 2, 80, (0, 0), 0, None, None),        # only its own key
     (1, 5, 64, 2, 1, 256, (-1, -1), 0, None, None),
+    (1, 2, 200, 2, 1, 32, (20, 0), 5, None, None),        # most of the cache out of sight, its first keys not
     (2, 2, 700, 2, 1, 16, (600, 0), 3, None, (700, 40)),  # keys split over workgroups, one of them without any
 ]

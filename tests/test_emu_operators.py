@@ -109,6 +109,8 @@ def test_attention(emu, b, sq, sk, hq, hk, dh, window, sinks, ql, kl, dtype):  #
     for s in range(b):   # what lies past a sequence's keys must not matter
         if kl is not None:
             hold_k[s, kl[s]:], hold_v[s, kl[s]:] = np.nan, np.inf
+        seen = C.seen_keys(sq if ql is None else ql[s], sk if kl is None else kl[s], sk, window, sinks)
+        hold_k[s, ~seen], hold_v[s, ~seen] = np.inf, np.nan   # nor keys that no query sees
     bufs = [buf(emu, t, dtype) for t in (q, hold_k, hold_v, np.full(q.shape, 7.0, np.float32))]
     lens = [run_emu.Buf(emu, np.array(n, np.int32)) if n is not None else None for n in (ql, kl)]
     a = pwdec.AttentionArgs(b, sq, sk, hq, hk, dh, CODE[dtype])

@@ -200,6 +200,9 @@ def test_attention(b, sq, sk, hq, hk, dh, window, sinks, ql, kl, dtype):
     for s in range(b):   # what lies past a sequence's keys must not matter
         if kl is not None:
             cache[s, kl[s]:, 0], cache[s, kl[s]:, 1] = float("nan"), float("inf")
+        seen = C.seen_keys(sq if ql is None else ql[s], sk if kl is None else kl[s], sk, window, sinks)
+        hidden = torch.from_numpy(~seen).cuda()
+        cache[s, :sk, 0][hidden], cache[s, :sk, 1][hidden] = float("inf"), float("nan")   # nor keys that no query sees
     out = torch.full((b, sq, hq, dh), 7.0, dtype=DT[dtype], device="cuda")
     lens = [dev(np.array(n, np.int32)) if n is not None else None for n in (ql, kl)]
     pwdec.attention(dev(q, dtype), cache[:, :sk, 0], cache[:, :sk, 1], out, window=window, sinks=sinks, q_lengths=lens[0],
